@@ -396,7 +396,7 @@ def _run_own(st):
     if kind == "fork":
         cache.free(st["dst"])                # the copies of the pass before
         cache.fork(st["src"], st["dst"])
-        cache.append(st["rows_k"], st["rows_v"], st["row_start"], st["max_rows"], mask=st["mask"], node=st["node"])
+        cache.append(st["rows_k"], st["rows_v"], st["row_start"], mask=st["mask"], node=st["node"])
         return st["k"], st["v"], st["refs"], st["table"], st["len"]
     st["ints"].copy_(st["ints0"])            # as it was before the sequences ended
     cache.free(st["gone"])
