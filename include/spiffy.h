@@ -372,6 +372,115 @@ int spiffy_subgraph_search(const int64_t *count, const int32_t *level, int32_t N
                            int32_t D, uint64_t *best_mask, int64_t *best_sum, uint64_t *n_connected,
                            int32_t *nodes_out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Paged cache: pages that sequences share, attention of drafted token trees over them ----
+ *
+ * A layer's cache is a pool of n_pages pages of page_size rows, k and v each [n_pages, Hkv, page_size, hd].  Row table
+ * [s, 0 .. ceil(len[s] / page_size) - 1] names the pages of sequence s in order: cache row j of s (sequence position j, keys already
+ * rotated) is row j % page_size of page table[s, j / page_size].  All layers have the same table.  refs[p] is the number of
+ * table entries that name page p, 0 = free.  A page that is not full belongs to one sequence only (spiffy_pages_fork copies it), so an
+ * append never writes what another sequence reads.  An empty cache has refs 0, len 0 and table -1 everywhere.
+ * The three arrays are DEVICE memory, only the spiffy_pages_* calls change them, in stream order, without the host: calls that
+ * change the same cache must not overlap, and none that reads it may overlap one that changes it.  A table entry outside [0, n_pages) is
+ * taken for a page without rows, len is taken within [0, max_pages * page_size]; nothing is read or written out of range for either.
+ *
+ * New rows of all sequences lie one behind the other: rows row_start[s] .. row_start[s+1]-1 belong to sequence s (row_start [n_seqs+1],
+ * device, ascending; values are taken within [0, T], an end in front of its start as no rows).  Rows from row_start[n_seqs] on
+ * belong to none: outputs there are left as they were.
+ * A tree is given by mask [T, mask_words] of 64-bit words: bit i % 64 of word i / 64 of row t says that row t attends to the i-th new
+ * row of its own sequence (a drafted token: to its ancestors and itself; a state of a block: to the state's rows).
+ *
+ * Of cfg only n_q_heads (<= 4096), n_kv_heads, head_dim (a multiple of 8, <= 256) and dtype count.  n_seqs <= SPIFFY_MAX_SEQS,
+ * n_pages <= 2^30, max_pages <= 2^22, n_sel <= 2^22, rows of the pool, of a table row and of a selection below 2^31,
+ * 1 <= T <= SPIFFY_MAX_NEW_ROWS: SPIFFY_ESHAPE beyond.  Buffers that a call writes may not overlap those that it reads. */
+#define SPIFFY_MAX_SEQS 4096
+#define SPIFFY_MAX_NEW_ROWS (1 << 20)
+#define SPIFFY_MAX_TREE 1024     /* new rows of one sequence in an attention or under a mask */
+#define SPIFFY_MAX_PAGED_LAYERS 256
+
+typedef struct {
+  void *k, *v;     /* one layer's pool */
+  void *summary;   /* [n_pages, Hkv, 2, hd] of the same type: least and greatest key of a page by channel; NULL = not kept */
+} spiffy_page_layer;
+
+typedef struct {
+  int32_t n_pages, page_size;
+  int32_t n_seqs, max_pages;
+  int32_t *refs;    /* [n_pages] */
+  int32_t *table;   /* [n_seqs, max_pages] */
+  int32_t *len;     /* [n_seqs] */
+} spiffy_paged_cache;
+
+/* What became of one sequence (append) or pair (fork); a sequence or pair that is not done is left as it was. */
+enum { SPIFFY_PAGES_DONE = 0, SPIFFY_PAGES_NO_PAGE = 1 /* too few free pages */, SPIFFY_PAGES_NO_ENTRY = 2 /* too few table entries */,
+       SPIFFY_PAGES_BAD = 3 /* an index out of range, a destination that is not empty, a last page that is shared or none */ };
+
+/* Bytes of scratch for any of the spiffy_pages_* calls on this cache; 0 on invalid arguments. */
+size_t spiffy_pages_workspace_bytes(const spiffy_paged_cache *cache);
+
+/* Accepted rows to the end of their sequences, in every layer.  rows_k / rows_v: HOST arrays of n_layers device pointers to rows of
+ * Hkv * hd elements, row_stride elements apart (k already rotated).  mask and node both NULL: every new row of a sequence is
+ * appended, in order.  With mask (as above) and node [n_seqs] (device, node_stride apart, e.g. the nodes of n_seqs
+ * spiffy_accept_result): of sequence s the rows whose bits are set in mask row row_start[s] + node[s], ascending: the path to the
+ * accepted node; node[s] < 0 appends nothing.  Pages are taken as needed, the lowest free ones, in the order of sequences and rows; a
+ * sequence for which too few are left gets none of its rows, and those behind it are tried.  status [n_seqs] (device) may be NULL.
+ * k, v of the layers, refs, table and len are written; summaries are not (spiffy_page_summary). */
+int spiffy_pages_append(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t n_layers, const spiffy_page_layer *layers,
+                        const void *const *rows_k, const void *const *rows_v, int64_t row_stride, const int32_t *row_start, int32_t T,
+                        const uint64_t *mask, int32_t mask_words, const int32_t *node, int32_t node_stride, int32_t *status,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Sequence dst[i] becomes a copy of sequence src[i], i = 0 .. n-1 (device arrays), in every layer: full pages are shared, the rows of
+ * a last page that is not full are copied to the lowest free page (summaries of the layers that keep them too).  All sources are read as
+ * they were before the call.  dst[i] must be empty (len 0) and be named by no earlier pair, otherwise the pair is SPIFFY_PAGES_BAD.
+ * n <= SPIFFY_MAX_SEQS.  status [n] (device) may be NULL. */
+int spiffy_pages_fork(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t n_layers, const spiffy_page_layer *layers,
+                      const int32_t *src, const int32_t *dst, int32_t n, int32_t *status, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/* Sequences seqs[0 .. n-1] (device) become empty: len 0, their table entries -1, one reference less to each of their pages.  An index out
+ * of range is passed over, one that comes twice counts once.  n <= SPIFFY_MAX_SEQS. */
+int spiffy_pages_free(const spiffy_paged_cache *cache, const int32_t *seqs, int32_t n, void *stream);
+
+/* The pages in use take the ids 0 .. *n_used - 1: those above, in ascending order, move to the free ids below, in ascending order, in
+ * every layer (with their summaries where kept); refs and table follow.  n_used (device, may be NULL). */
+int spiffy_pages_compact(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t n_layers, const spiffy_page_layer *layers,
+                         int32_t *n_used, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Summaries of the pages of every sequence s that hold rows start[s] .. len[s]-1 (start [n_seqs], device; NULL = 0 everywhere): the least
+ * and the greatest value of each channel over the rows in use of a page.  Other summaries are left as they were. */
+int spiffy_page_summary(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t n_layers, const spiffy_page_layer *layers,
+                        const int32_t *start, void *stream);
+
+/* The pages that a kv head of a sequence is to read.  A page's score is a bound on what any of its keys can score with any of the new
+ * rows of the sequence and the query heads of the kv head: max over (row, head) of sum_c max(q_c lo_c, q_c hi_c), summed in 64 bits, so
+ * that which of two pages is higher does not depend on the order of a sum.  The first keep_first and the last keep_last pages of a
+ * sequence count as the highest, then the higher score, equal ones to the lower index; a score that is NaN is the lowest.
+ * q: T rows of Hq * hd elements, q_stride apart.  selected [n_seqs, Hkv, n_sel] (device): indices into the sequence's table row,
+ * ascending, min(n_sel, pages in use) of them, -1 behind.  A sequence without new rows selects by index alone (every score is
+ * the lowest).  n_sel >= 1, keep_first, keep_last >= 0; new rows of a sequence <= SPIFFY_MAX_TREE, max_rows is a bound on them
+ * that the caller knows (rows beyond do not count). */
+size_t spiffy_page_select_workspace_bytes(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache);
+int spiffy_page_select(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, const spiffy_page_layer *layer, const void *q,
+                       int64_t q_stride, const int32_t *row_start, int32_t T, int32_t max_rows, int32_t n_sel, int32_t keep_first,
+                       int32_t keep_last, int32_t *selected, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of the new rows over the cache: row t of sequence s and query head h attends to the rows of the cache of s and to the new
+ * rows that its mask names (mask NULL: to all new rows of s): out = sum_j w_j v_j, w = softmax(scale * q . k_j).  n_seqs trees of
+ * different sizes in one call; one new row without cache or mask, a chain, a tree, the states of a block are all the same call.
+ * selected [n_seqs, Hkv, n_sel] (NULL = all pages; as spiffy_page_select leaves it): of the cache only the rows of these pages, in any
+ * order, entries outside the pages in use are passed over, each page named once.
+ * q rows of Hq * hd, k and v rows of Hkv * hd elements, q_stride / kv_stride apart (one buffer of q | k | v rows will do); out
+ * rows out_stride apart; strides are multiples of 16 bytes (SPIFFY_EALIGN).  scale is finite.  max_rows <= SPIFFY_MAX_TREE: a bound
+ * on the new rows of a sequence; rows beyond it are left as they were.
+ * Keys and values that a row does not attend to do not show in it, whatever they hold (NaN, infinities).  A row that attends to
+ * nothing, or whose scores are all minus infinity, gets zeros.  Sums and softmax statistics are fp32; in bf16 the probabilities are
+ * rounded to bf16 for the product with the values. */
+size_t spiffy_tree_attention_workspace_bytes(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t T, int32_t max_rows);
+int spiffy_tree_attention(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, const spiffy_page_layer *layer, const void *q,
+                          int64_t q_stride, const void *k, const void *v, int64_t kv_stride, const int32_t *row_start, int32_t T,
+                          int32_t max_rows, const uint64_t *mask, int32_t mask_words, const int32_t *selected, int32_t n_sel, float scale,
+                          void *out, int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

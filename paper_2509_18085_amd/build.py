@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libspiffy.so")
 SOURCES = ["api.hip", "generic_kernels.hip", "tile_gemm.hip", "tile_attn.hip", "graph_accept.hip", "draft_prune.hip", "head_topk.hip", "subgraph_search.hip", "mfma_gemm.hip",
-           "mfma_gemm_swiglu.hip", "mfma_gemm_qkv.hip", "mfma_gemm_partial.hip", "mfma_gemm_store.hip", "mfma_gemm_head.hip", "mfma_attn.hip"]
+           "mfma_gemm_swiglu.hip", "mfma_gemm_qkv.hip", "mfma_gemm_partial.hip", "mfma_gemm_store.hip", "mfma_gemm_head.hip", "mfma_attn.hip", "api_paged.hip", "paged_pages.hip", "paged_select.hip", "paged_attn.hip"]
 PROBE_LIB = os.path.join(HERE, "libspiffy_probe.so")     # bench-only: measured peaks of the machine (csrc/probe.hip)
 # -ffp-contract=on: a multiply and an add are fused only where the source writes them in one expression, so the
 # rounding of a kernel does not depend on how the optimiser inlined or ordered it (different instantiations of one
@@ -73,7 +73,7 @@ def assembly(source: str) -> str:
 
 
 def build_host_sanitized() -> tuple:
-    """The same library with the HOST code of the launcher (csrc/api.hip: argument checks, workspace carving, kernel
+    """The same library with the HOST code of the launcher (csrc/api.hip, csrc/api_paged.hip: argument checks, workspace carving, kernel
     selection) compiled under AddressSanitizer and UndefinedBehaviorSanitizer; device code and the kernel translation
     units are the normal ones.  Returns (library path, sanitizer runtime to preload).  For the CPU tests only."""
     if not all(os.path.exists(os.path.join(OBJ, s.replace(".hip", ".o"))) for s in SOURCES):
@@ -81,12 +81,14 @@ def build_host_sanitized() -> tuple:
     out_dir = os.path.join(OBJ, "asan")
     os.makedirs(out_dir, exist_ok=True)
     hipcc = _hipcc()
-    api_o = os.path.join(out_dir, "api.o")
+    host = ["api.hip", "api_paged.hip"]
+    host_o = [os.path.join(out_dir, s.replace(".hip", ".o")) for s in host]
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host",
            "-fno-sanitize-recover=undefined"]
     flags = [f if f != "-O3" else "-O1" for f in FLAGS] + ["-g"]
-    _run([hipcc] + flags + san + ["-c", os.path.join(CSRC, "api.hip"), "-o", api_o])
-    objs = [api_o] + [os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES if s != "api.hip"]
+    for s, o in zip(host, host_o):
+        _run([hipcc] + flags + san + ["-c", os.path.join(CSRC, s), "-o", o])
+    objs = host_o + [os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES if s not in host]
     lib = os.path.join(out_dir, "libspiffy_asan.so")
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-fsanitize=address,undefined", "-o", lib] + objs)
     clang = os.path.join(os.path.dirname(os.path.realpath(hipcc)), "..", "lib", "llvm", "bin", "clang")

@@ -28,9 +28,13 @@ EXPORTS = ["spiffy_status_str", "spiffy_uses_mfma", "spiffy_workspace_bytes", "s
            "spiffy_subgraph_search_workspace_bytes", "spiffy_subgraph_search", "spiffy_verify_step",
            "spiffy_workspace_bytes_seq", "spiffy_verify_step_seq", "spiffy_workspace_bytes_commit",
            "spiffy_verify_step_commit", "spiffy_decode_head_static", "spiffy_gemm_plan", "spiffy_layer_gemm_plan",
-           "spiffy_layer_gemm"]
+           "spiffy_layer_gemm", "spiffy_pages_workspace_bytes", "spiffy_pages_append", "spiffy_pages_fork", "spiffy_pages_free",
+           "spiffy_pages_compact", "spiffy_page_summary", "spiffy_page_select_workspace_bytes", "spiffy_page_select",
+           "spiffy_tree_attention_workspace_bytes", "spiffy_tree_attention"]
 GEMM_STORE, GEMM_RESID, GEMM_SWIGLU = 0, 1, 2
 TAIL_MASKED = -2
+MAX_SEQS, MAX_NEW_ROWS, MAX_TREE = 4096, 1 << 20, 1024
+PAGES_DONE, PAGES_NO_PAGE, PAGES_NO_ENTRY, PAGES_BAD = 0, 1, 2, 3
 
 
 class ModelCfg(C.Structure):
@@ -51,6 +55,15 @@ class PrefixKV(C.Structure):
 
 class AcceptResult(C.Structure):
     _fields_ = [("node", C.c_int32), ("depth", C.c_int32), ("n_steps", C.c_int32), ("flags", C.c_int32)]
+
+
+class PageLayer(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("summary", C.c_void_p)]
+
+
+class PagedCacheStruct(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("refs", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p)]
 
 
 class GemmLaunch(C.Structure):
@@ -132,6 +145,29 @@ def _load() -> C.CDLL:
     lib.spiffy_verify_step.argtypes = [cfgp, i32, C.POINTER(LayerWeights), C.POINTER(PrefixKV), vp, vp, vp, vp,
                                        i32, i32, i32, vp, i32, i32, f32, f32, i32, vp, vp, vp, vp, vp, vp, vp,
                                        vp, vp, sz, vp]
+    i64, cachep, layerp = C.c_int64, C.POINTER(PagedCacheStruct), C.POINTER(PageLayer)
+    lib.spiffy_pages_workspace_bytes.restype = sz
+    lib.spiffy_pages_workspace_bytes.argtypes = [cachep]
+    lib.spiffy_pages_append.restype = C.c_int
+    lib.spiffy_pages_append.argtypes = [cfgp, cachep, i32, layerp, C.POINTER(vp), C.POINTER(vp), i64, vp, i32, vp, i32, vp, i32, vp,
+                                        vp, sz, vp]
+    lib.spiffy_pages_fork.restype = C.c_int
+    lib.spiffy_pages_fork.argtypes = [cfgp, cachep, i32, layerp, vp, vp, i32, vp, vp, sz, vp]
+    lib.spiffy_pages_free.restype = C.c_int
+    lib.spiffy_pages_free.argtypes = [cachep, vp, i32, vp]
+    lib.spiffy_pages_compact.restype = C.c_int
+    lib.spiffy_pages_compact.argtypes = [cfgp, cachep, i32, layerp, vp, vp, sz, vp]
+    lib.spiffy_page_summary.restype = C.c_int
+    lib.spiffy_page_summary.argtypes = [cfgp, cachep, i32, layerp, vp, vp]
+    lib.spiffy_page_select_workspace_bytes.restype = sz
+    lib.spiffy_page_select_workspace_bytes.argtypes = [cfgp, cachep]
+    lib.spiffy_page_select.restype = C.c_int
+    lib.spiffy_page_select.argtypes = [cfgp, cachep, layerp, vp, i64, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+    lib.spiffy_tree_attention_workspace_bytes.restype = sz
+    lib.spiffy_tree_attention_workspace_bytes.argtypes = [cfgp, cachep, i32, i32]
+    lib.spiffy_tree_attention.restype = C.c_int
+    lib.spiffy_tree_attention.argtypes = [cfgp, cachep, layerp, vp, i64, vp, vp, i64, vp, i32, i32, vp, i32, vp, i32, C.c_float, vp, i64,
+                                          vp, sz, vp]
     return lib
 
 
@@ -551,3 +587,225 @@ class SeqStepPlan(StepPlan):
             _ptr(o["target_states"]), _ptr(o["result"]), _ptr(o["accepted_state"]), wp, wn, _stream(stream)),
             "spiffy_verify_step_seq")
         return o
+
+
+def tree_mask(edges, n: int, device="cuda") -> torch.Tensor:
+    """Masks of the n nodes of one draft graph, [n, ceil(n / 64)] int64 (bit i % 64 of word i / 64): every node attends to itself and to all
+    its ancestors.  edges: (parent, child) rows with parent < child, as graph_accept takes them (a sequence or a tensor; host
+    arithmetic: a graph's masks are made once)."""
+    rows = [1 << i for i in range(n)]
+    for p, c in sorted(((int(p), int(c)) for p, c in (edges.tolist() if isinstance(edges, torch.Tensor) else edges)), key=lambda e: e[1]):
+        if not 0 <= p < c < n:
+            raise ValueError("an edge goes from a node to a later one: got (%d, %d) of %d nodes" % (p, c, n))
+        rows[c] |= rows[p]
+    words = [[r >> 64 * w & (1 << 64) - 1 for w in range((n + 63) // 64)] for r in rows]
+    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in words], dtype=torch.int64, device=device)
+
+
+class PagedCache:
+    """A cache of pages that sequences share, and the attention of drafted token trees over it (spiffy_pages_*, spiffy_page_*,
+    spiffy_tree_attention).
+
+    k, v [n_layers, n_pages, Hkv, page_size, hd] in cfg's type, refs [n_pages], table [n_seqs, max_pages] and len [n_seqs] int32, summary
+    (optional) [n_layers, n_pages, Hkv, 2, hd]: contiguous tensors on one device, kept as they are.  `empty` makes them.  New rows
+    of all sequences lie one behind the other, row_start [n_seqs + 1] int32 says where those of each begin; max_rows is a bound on
+    the new rows of one sequence.  Nothing waits for the device.  Outputs and workspaces that the caller does not pass are
+    allocated by the call, so calls that only read the cache may run at the same time on several streams."""
+
+    def __init__(self, cfg: ModelCfg, k: torch.Tensor, v: torch.Tensor, refs: torch.Tensor, table: torch.Tensor, len: torch.Tensor,
+                 summary: Optional[torch.Tensor] = None):
+        if k.dim() != 5 or k.shape != v.shape or k.shape[2] != cfg.n_kv_heads or k.shape[4] != cfg.head_dim:
+            raise ValueError("k and v are [n_layers, n_pages, Hkv, page_size, hd]")
+        if table.dim() != 2 or refs.shape != k.shape[1:2] or len.shape != table.shape[:1]:
+            raise ValueError("refs is [n_pages], table [n_seqs, max_pages], len [n_seqs]")
+        if summary is not None and tuple(summary.shape) != (*k.shape[:3], 2, k.shape[4]):
+            raise ValueError("summary is [n_layers, n_pages, Hkv, 2, hd]")
+        self.device, self._dt = k.device, _tdtype(cfg)
+        for t in (k, v) if summary is None else (k, v, summary):
+            self._typed(t, self._dt)
+        for t in (refs, table, len):
+            self._typed(t, torch.int32)
+        self.cfg, self.k, self.v, self.refs, self.table, self.len, self.summary = cfg, k, v, refs, table, len, summary
+        self.n_layers, self.n_pages, _, self.page_size, _ = k.shape
+        self.n_seqs, self.max_pages = table.shape
+        self._struct = PagedCacheStruct(self.n_pages, self.page_size, self.n_seqs, self.max_pages, _ptr(refs), _ptr(table), _ptr(len))
+        step, sstep = k.stride(0) * k.element_size(), 0 if summary is None else summary.stride(0) * k.element_size()
+        self._layers = (PageLayer * max(1, self.n_layers))(*[PageLayer(_ptr(k) + l * step, _ptr(v) + l * step, None if summary is None else _ptr(summary) + l * sstep)
+                                                             for l in range(self.n_layers)])
+        self._cfg, self._cache = C.byref(self.cfg), C.byref(self._struct)
+        self._pages_ws = int(lib.spiffy_pages_workspace_bytes(self._cache))
+        self._select_ws = int(lib.spiffy_page_select_workspace_bytes(self._cfg, self._cache))
+        if not self._pages_ws or not self._select_ws:
+            raise SpiffyError(SPIFFY_ESHAPE, "PagedCache")
+        self._attn_ws: Dict[Tuple[int, int], int] = {}
+
+    @classmethod
+    def empty(cls, cfg: ModelCfg, n_layers: int, n_pages: int, page_size: int, n_seqs: int, max_pages: int, *, summaries: bool = False,
+              device="cuda") -> "PagedCache":
+        shape, dt = (n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim), _tdtype(cfg)
+        make = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)
+        return cls(cfg, torch.empty(shape, dtype=dt, device=device), torch.empty(shape, dtype=dt, device=device), make(n_pages),
+                   make(n_seqs, max_pages).fill_(-1), make(n_seqs),
+                   torch.zeros((*shape[:3], 2, shape[4]), dtype=dt, device=device) if summaries else None)
+
+    # -- arguments -------------------------------------------------------------------------------------------------------------
+
+    def _typed(self, t: torch.Tensor, dtype) -> Optional[int]:
+        if t.dtype != dtype or t.device != self.device:
+            raise ValueError("expected %s on %s, got %s on %s" % (dtype, self.device, t.dtype, t.device))
+        return _ptr(t)
+
+    def _ints(self, t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
+        if t is None:
+            return None
+        if t.dim() != 1 or (n is not None and t.shape[0] != n):
+            raise ValueError("expected [%s] int32, got %s" % ("n" if n is None else n, tuple(t.shape)))
+        return self._typed(t, torch.int32)
+
+    def _rows(self, t: torch.Tensor, heads: int, T: Optional[int] = None) -> int:
+        """[T, heads, hd] with rows of any stride; the heads of a row lie side by side."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or (T is not None and t.shape[0] != T):
+            raise ValueError("expected [%s, %d, %d], got %s" % ("T" if T is None else T, heads, self.cfg.head_dim, tuple(t.shape)))
+        if t.dtype != self._dt or t.device != self.device:
+            raise ValueError("expected %s on %s, got %s on %s" % (self._dt, self.device, t.dtype, t.device))
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.cfg.head_dim):
+            raise ValueError("the heads of a row lie side by side")
+        return self._stride(t, 0, heads)
+
+    def _stride(self, t: torch.Tensor, dim: int, heads: int) -> int:
+        return t.stride(dim) if t.shape[dim] > 1 else heads * self.cfg.head_dim      # of one row torch may say anything
+
+    def _mask(self, mask: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
+        if mask is None:
+            return None, 0
+        if mask.dim() != 2 or mask.shape[0] != T:
+            raise ValueError("mask is [T, words] int64")
+        return self._typed(mask, torch.int64), mask.shape[1]
+
+    def _layer(self, layer: int):
+        if not 0 <= layer < self.n_layers:
+            raise IndexError("layer %d of %d" % (layer, self.n_layers))
+        return C.byref(self._layers[layer])
+
+    def _call(self, workspace_bytes: int, workspace: Optional[torch.Tensor], stream, call):
+        """call(workspace pointer, its bytes, stream) on the cache's device, in the stream's allocator."""
+        with torch.cuda.device(self.device):
+            if stream is not None and not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=self.device) if int(stream) else torch.cuda.default_stream(self.device)
+            with torch.cuda.stream(stream):                       # None: the current one
+                if workspace is None and workspace_bytes:
+                    workspace = torch.empty(workspace_bytes + 256, dtype=torch.uint8, device=self.device)
+                return call(*(_ws(workspace) if workspace is not None else (None, 0)), _stream())
+
+    # -- pages -----------------------------------------------------------------------------------------------------------------
+
+    def append(self, rows_k: torch.Tensor, rows_v: torch.Tensor, row_start: torch.Tensor, mask: Optional[torch.Tensor] = None,
+               node: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> None:
+        """New rows [n_layers, T, Hkv, hd] to the end of their sequences: all of them, or with mask [T, words] and node [n_seqs] (for
+        instance result[:, 0] of n_seqs walks) those on the path to each sequence's accepted node; node -1 appends nothing.
+        status [n_seqs] int32 receives PAGES_*."""
+        if rows_k.dim() != 4 or rows_k.shape != rows_v.shape or rows_k.shape[0] != self.n_layers or rows_k.stride() != rows_v.stride():
+            raise ValueError("rows_k and rows_v are [n_layers, T, Hkv, hd] of the same strides")
+        T, words = rows_k.shape[1], 0
+        self._ints(row_start, self.n_seqs + 1)
+        if T == 0:
+            return
+        stride = self._rows(rows_k[0], self.cfg.n_kv_heads)
+        self._rows(rows_v[0], self.cfg.n_kv_heads)
+        mp, words = self._mask(mask, T)
+        if node is not None and (node.dtype != torch.int32 or node.device != self.device or tuple(node.shape) != (self.n_seqs,)):
+            raise ValueError("node is [n_seqs] int32")
+        node_stride = 1 if node is None or self.n_seqs == 1 else node.stride(0)
+        step = rows_k.stride(0) * rows_k.element_size()
+        kp = (C.c_void_p * self.n_layers)(*[rows_k.data_ptr() + l * step for l in range(self.n_layers)])
+        vp = (C.c_void_p * self.n_layers)(*[rows_v.data_ptr() + l * step for l in range(self.n_layers)])
+        self._call(self._pages_ws, workspace, stream, lambda wp, wn, st: _check(lib.spiffy_pages_append(
+            self._cfg, self._cache, self.n_layers, self._layers, kp, vp, stride, _ptr(row_start), T, mp, words,
+            None if node is None else node.data_ptr(), node_stride, self._ints(status, self.n_seqs), wp, wn, st), "spiffy_pages_append"))
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+             stream=None) -> None:
+        """Empty sequences dst [n] become copies of sequences src [n] (int32): full pages are shared, a last one that is not full is copied."""
+        n = src.shape[0]
+        sp, dp, tp = self._ints(src), self._ints(dst, n), self._ints(status, n)
+        if n:
+            self._call(self._pages_ws, workspace, stream, lambda wp, wn, st: _check(lib.spiffy_pages_fork(
+                self._cfg, self._cache, self.n_layers, self._layers, sp, dp, n, tp, wp, wn, st), "spiffy_pages_fork"))
+
+    def free(self, seqs: torch.Tensor, stream=None) -> None:
+        """Sequences seqs [n] (int32) become empty, their pages lose a reference."""
+        sp = self._ints(seqs)
+        if seqs.shape[0]:
+            self._call(0, None, stream, lambda wp, wn, st: _check(lib.spiffy_pages_free(self._cache, sp, seqs.shape[0], st), "spiffy_pages_free"))
+
+    def compact(self, n_used: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The pages in use move to the lowest ids; returns how many they are, [1] int32."""
+        def call(wp, wn, st):
+            out = torch.empty(1, dtype=torch.int32, device=self.device) if n_used is None else n_used
+            _check(lib.spiffy_pages_compact(self._cfg, self._cache, self.n_layers, self._layers, self._ints(out, 1), wp, wn, st),
+                   "spiffy_pages_compact")
+            return out
+        return self._call(self._pages_ws, workspace, stream, call)
+
+    # -- attention -------------------------------------------------------------------------------------------------------------
+
+    def summarize(self, start: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Brings `summary` up to date for the pages that hold rows start[s] .. len[s]-1 (None: all rows)."""
+        sp = self._ints(start, self.n_seqs)
+        self._call(0, None, stream, lambda wp, wn, st: _check(lib.spiffy_page_summary(self._cfg, self._cache, self.n_layers, self._layers, sp, st),
+                                                             "spiffy_page_summary"))
+
+    def select(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int, n_sel: int, keep_first: int = 0, keep_last: int = 1,
+               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The n_sel pages of every (sequence, kv head) whose summaries promise the highest scores with the new rows' queries q
+        [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; its first keep_first and last keep_last pages come before all others."""
+        lp, stride, rp = self._layer(layer), self._rows(q, self.cfg.n_q_heads), self._ints(row_start, self.n_seqs + 1)
+        shape = (self.n_seqs, self.cfg.n_kv_heads, n_sel)
+        if out is not None and tuple(out.shape) != shape:
+            raise ValueError("out is %s" % (shape,))
+
+        def call(wp, wn, st):
+            o = torch.empty(shape, dtype=torch.int32, device=self.device) if out is None else out
+            _check(lib.spiffy_page_select(self._cfg, self._cache, lp, q.data_ptr(), stride, rp, q.shape[0], max_rows, n_sel, keep_first,
+                                          keep_last, self._typed(o, torch.int32), wp, wn, st), "spiffy_page_select")
+            return o
+        return self._call(self._select_ws, workspace, stream, call)
+
+    def attend_workspace_bytes(self, T: int, max_rows: int) -> int:
+        n = self._attn_ws.get((T, max_rows))
+        if n is None:
+            n = int(lib.spiffy_tree_attention_workspace_bytes(self._cfg, self._cache, T, max_rows))
+            if n == 0:
+                raise SpiffyError(SPIFFY_EINVAL, "spiffy_tree_attention_workspace_bytes")
+            self._attn_ws[(T, max_rows)] = n
+        return n
+
+    def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
+               mask: Optional[torch.Tensor] = None, selected: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention of the new rows q [T, Hq, hd] over their sequences' cache rows and over the new rows k, v [T, Hkv, hd] that mask
+        [T, words] names (None: all of the sequence); rows may be strided views of one q | k | v buffer.  selected: only these pages of
+        the cache (see select).  Returns [T, Hq, hd]; rows behind row_start[-1] are not written."""
+        Hq, Hkv, T = self.cfg.n_q_heads, self.cfg.n_kv_heads, q.shape[0]
+        lp, qs, ks, vs = self._layer(layer), self._rows(q, Hq), self._rows(k, Hkv, T), self._rows(v, Hkv, T)
+        if ks != vs:
+            raise ValueError("rows of k and v have the same stride")
+        rp, (mp, words), n_sel, os_ = self._ints(row_start, self.n_seqs + 1), self._mask(mask, T), 0, Hq * self.cfg.head_dim
+        if selected is not None:
+            if selected.dim() != 3 or tuple(selected.shape[:2]) != (self.n_seqs, Hkv):
+                raise ValueError("selected is [n_seqs, Hkv, n_sel]")
+            n_sel = selected.shape[2]
+        selp = None if selected is None else self._typed(selected, torch.int32)
+        if out is not None:
+            os_ = self._rows(out, Hq, T)
+        if T == 0:
+            return torch.empty_like(q) if out is None else out
+
+        def call(wp, wn, st):
+            o = torch.empty((T, Hq, self.cfg.head_dim), dtype=self._dt, device=self.device) if out is None else out
+            _check(lib.spiffy_tree_attention(self._cfg, self._cache, lp, q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks, rp, T, max_rows,
+                                             mp, words, selp, n_sel, self.cfg.head_dim ** -0.5 if scale is None else scale, o.data_ptr(), os_,
+                                             wp, wn, st), "spiffy_tree_attention")
+            return o
+        return self._call(self.attend_workspace_bytes(T, max_rows), workspace, stream, call)
