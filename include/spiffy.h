@@ -390,8 +390,8 @@ int spiffy_subgraph_search(const int64_t *count, const int32_t *level, int32_t N
  * row of its own sequence (a drafted token: to its ancestors and itself; a state of a block: to the state's rows).
  *
  * Of cfg only n_q_heads (<= 4096), n_kv_heads, head_dim (a multiple of 8, <= 256) and dtype count.  n_seqs <= SPIFFY_MAX_SEQS,
- * n_pages <= 2^30, max_pages <= 2^22, n_sel <= 2^22, rows of the pool, of a table row and of a selection below 2^31,
- * 1 <= T <= SPIFFY_MAX_NEW_ROWS: SPIFFY_ESHAPE beyond.  Buffers that a call writes may not overlap those that it reads. */
+ * n_pages <= 2^30, max_pages <= 2^22, n_sel <= 2^22, rows of the pool below 2^31, of a table row and of a selection up to
+ * 2^31 - 2^16, 1 <= T <= SPIFFY_MAX_NEW_ROWS: SPIFFY_ESHAPE beyond.  Buffers that a call writes may not overlap those that it reads. */
 #define SPIFFY_MAX_SEQS 4096
 #define SPIFFY_MAX_NEW_ROWS (1 << 20)
 #define SPIFFY_MAX_TREE 1024     /* new rows of one sequence in an attention or under a mask */
@@ -471,11 +471,12 @@ int spiffy_page_select(const spiffy_model_cfg *cfg, const spiffy_paged_cache *ca
  * order, entries outside the pages in use are passed over, each page named once.
  * q rows of Hq * hd, k and v rows of Hkv * hd elements, q_stride / kv_stride apart (one buffer of q | k | v rows will do); out
  * rows out_stride apart; strides are multiples of 16 bytes (SPIFFY_EALIGN).  scale is finite.  max_rows <= SPIFFY_MAX_TREE: a bound
- * on the new rows of a sequence; rows beyond it are left as they were.
+ * on the new rows of a sequence; rows beyond it are left as they were.  n_seqs * n_q_heads * max_rows / 16 has to stay below some 2^22
+ * (SPIFFY_ESHAPE).
  * Keys and values that a row does not attend to do not show in it, whatever they hold (NaN, infinities).  A row that attends to
  * nothing, or whose scores are all minus infinity, gets zeros.  Sums and softmax statistics are fp32; in bf16 the probabilities are
  * rounded to bf16 for the product with the values. */
-size_t spiffy_tree_attention_workspace_bytes(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t T, int32_t max_rows);
+size_t spiffy_tree_attention_workspace_bytes(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t max_rows);
 int spiffy_tree_attention(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, const spiffy_page_layer *layer, const void *q,
                           int64_t q_stride, const void *k, const void *v, int64_t kv_stride, const int32_t *row_start, int32_t T,
                           int32_t max_rows, const uint64_t *mask, int32_t mask_words, const int32_t *selected, int32_t n_sel, float scale,

@@ -9,6 +9,7 @@ using namespace spiffy;
 namespace {
 
 constexpr int kMaxPoolPages = 1 << 30, kMaxTable = 1 << 22;
+constexpr int64_t kMaxPositions = (int64_t(1) << 31) - (1 << 16);      // rows of a sequence: kernels count some way past them in 31 bits
 
 inline bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 int dev(hipError_t e) { return e == hipSuccess ? SPIFFY_OK : SPIFFY_EDEVICE; }
@@ -25,7 +26,7 @@ Heads heads(const spiffy_model_cfg* c) { return Heads{c->n_q_heads, c->n_kv_head
 int check_sizes(const spiffy_paged_cache* c) {
   if (!c || c->n_pages < 1 || c->page_size < 1 || c->n_seqs < 1 || c->max_pages < 1) return SPIFFY_EINVAL;
   if (c->n_seqs > SPIFFY_MAX_SEQS || c->n_pages > kMaxPoolPages || c->max_pages > kMaxTable) return SPIFFY_ESHAPE;
-  if ((int64_t)c->n_pages * c->page_size > INT32_MAX || (int64_t)c->max_pages * c->page_size > INT32_MAX) return SPIFFY_ESHAPE;
+  if ((int64_t)c->n_pages * c->page_size > INT32_MAX || (int64_t)c->max_pages * c->page_size > kMaxPositions) return SPIFFY_ESHAPE;
   return SPIFFY_OK;
 }
 int check_cache(const spiffy_paged_cache* c) {
@@ -229,9 +230,9 @@ int spiffy_page_select(const spiffy_model_cfg* cfg, const spiffy_paged_cache* ca
   return dev(launch_page_select(a, (hipStream_t)stream));
 }
 
-size_t spiffy_tree_attention_workspace_bytes(const spiffy_model_cfg* cfg, const spiffy_paged_cache* cache, int32_t T, int32_t max_rows) {
-  if (check_heads(cfg) || check_sizes(cache) || T < 1 || T > SPIFFY_MAX_NEW_ROWS || max_rows < 1 || max_rows > SPIFFY_MAX_TREE) return 0;
-  return tree_attn_workspace_bytes(view(cache), heads(cfg), T, max_rows);
+size_t spiffy_tree_attention_workspace_bytes(const spiffy_model_cfg* cfg, const spiffy_paged_cache* cache, int32_t max_rows) {
+  if (check_heads(cfg) || check_sizes(cache) || max_rows < 1 || max_rows > SPIFFY_MAX_TREE) return 0;
+  return tree_attn_fits(view(cache), heads(cfg), max_rows) ? tree_attn_workspace_bytes(view(cache), heads(cfg), max_rows) : 0;
 }
 
 int spiffy_tree_attention(const spiffy_model_cfg* cfg, const spiffy_paged_cache* cache, const spiffy_page_layer* layer, const void* q,
@@ -244,8 +245,8 @@ int spiffy_tree_attention(const spiffy_model_cfg* cfg, const spiffy_paged_cache*
   if ((rc = check_rows(row_start, T, mask, mask_words))) return rc;
   if (max_rows > SPIFFY_MAX_TREE || (selected && n_sel > kMaxTable)) return SPIFFY_ESHAPE;
   const Heads h = heads(cfg);
-  // rows of the tables that the selection can name: positions are 31-bit numbers
-  if (selected && (int64_t)n_sel * cache->page_size > INT32_MAX) return SPIFFY_ESHAPE;
+  if (selected && (int64_t)n_sel * cache->page_size > kMaxPositions) return SPIFFY_ESHAPE;
+  if (!tree_attn_fits(view(cache), h, max_rows)) return SPIFFY_ESHAPE;
   const int es = h.f32 ? 4 : 2;
   if ((rc = check_stride(q_stride, (int64_t)h.Hq * h.hd, es)) || (rc = check_stride(kv_stride, (int64_t)h.Hkv * h.hd, es)) ||
       (rc = check_stride(out_stride, (int64_t)h.Hq * h.hd, es)))
@@ -253,7 +254,7 @@ int spiffy_tree_attention(const spiffy_model_cfg* cfg, const spiffy_paged_cache*
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(selected, 4)) return SPIFFY_EALIGN;
   TreeAttnArgs a{};
   a.c = view(cache);
-  if ((rc = check_workspace(workspace, workspace_bytes, tree_attn_workspace_bytes(a.c, h, T, max_rows)))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, tree_attn_workspace_bytes(a.c, h, max_rows)))) return rc;
   a.h = h;
   a.pk = layer->k;
   a.pv = layer->v;

@@ -96,7 +96,8 @@ struct TreeAttnArgs {
   float scale;
   void *out, *workspace;
 };
-size_t tree_attn_workspace_bytes(const PagedView& c, const Heads& h, int T, int max_rows);
+bool tree_attn_fits(const PagedView& c, const Heads& h, int max_rows);      // its workgroups
+size_t tree_attn_workspace_bytes(const PagedView& c, const Heads& h, int max_rows);
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st);
 
 // ---- device -----------------------------------------------------------------------------------------------------------------

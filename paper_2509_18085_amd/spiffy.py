@@ -164,7 +164,7 @@ def _load() -> C.CDLL:
     lib.spiffy_page_select.restype = C.c_int
     lib.spiffy_page_select.argtypes = [cfgp, cachep, layerp, vp, i64, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
     lib.spiffy_tree_attention_workspace_bytes.restype = sz
-    lib.spiffy_tree_attention_workspace_bytes.argtypes = [cfgp, cachep, i32, i32]
+    lib.spiffy_tree_attention_workspace_bytes.argtypes = [cfgp, cachep, i32]
     lib.spiffy_tree_attention.restype = C.c_int
     lib.spiffy_tree_attention.argtypes = [cfgp, cachep, layerp, vp, i64, vp, vp, i64, vp, i32, i32, vp, i32, vp, i32, C.c_float, vp, i64,
                                           vp, sz, vp]
@@ -637,7 +637,7 @@ class PagedCache:
         self._select_ws = int(lib.spiffy_page_select_workspace_bytes(self._cfg, self._cache))
         if not self._pages_ws or not self._select_ws:
             raise SpiffyError(SPIFFY_ESHAPE, "PagedCache")
-        self._attn_ws: Dict[Tuple[int, int], int] = {}
+        self._attn_ws: Dict[int, int] = {}
 
     @classmethod
     def empty(cls, cfg: ModelCfg, n_layers: int, n_pages: int, page_size: int, n_seqs: int, max_pages: int, *, summaries: bool = False,
@@ -772,13 +772,13 @@ class PagedCache:
             return o
         return self._call(self._select_ws, workspace, stream, call)
 
-    def attend_workspace_bytes(self, T: int, max_rows: int) -> int:
-        n = self._attn_ws.get((T, max_rows))
+    def attend_workspace_bytes(self, max_rows: int) -> int:
+        n = self._attn_ws.get(max_rows)
         if n is None:
-            n = int(lib.spiffy_tree_attention_workspace_bytes(self._cfg, self._cache, T, max_rows))
+            n = int(lib.spiffy_tree_attention_workspace_bytes(self._cfg, self._cache, max_rows))
             if n == 0:
-                raise SpiffyError(SPIFFY_EINVAL, "spiffy_tree_attention_workspace_bytes")
-            self._attn_ws[(T, max_rows)] = n
+                raise SpiffyError(SPIFFY_ESHAPE if max_rows > 0 else SPIFFY_EINVAL, "spiffy_tree_attention_workspace_bytes")
+            self._attn_ws[max_rows] = n
         return n
 
     def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
@@ -808,4 +808,4 @@ class PagedCache:
                                              mp, words, selp, n_sel, self.cfg.head_dim ** -0.5 if scale is None else scale, o.data_ptr(), os_,
                                              wp, wn, st), "spiffy_tree_attention")
             return o
-        return self._call(self.attend_workspace_bytes(T, max_rows), workspace, stream, call)
+        return self._call(self.attend_workspace_bytes(max_rows), workspace, stream, call)

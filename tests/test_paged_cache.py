@@ -569,7 +569,8 @@ def _host(**kw):
 
 
 BAD_CACHES = [(dict(n_pages=0), -1), (dict(page_size=0), -1), (dict(n_seqs=0), -1), (dict(max_pages=0), -1), (dict(n_seqs=4097), -2),
-              (dict(n_pages=1 << 27, page_size=16), -2), (dict(max_pages=(1 << 22) + 1, page_size=1), -2), (dict(max_pages=1 << 22, page_size=512), -2)]
+              (dict(n_pages=1 << 27, page_size=16), -2), (dict(max_pages=(1 << 22) + 1, page_size=1), -2), (dict(max_pages=1 << 22, page_size=512), -2),
+              (dict(max_pages=1 << 15, page_size=1 << 16), -2)]
 BAD_POINTERS = [(dict(refs=None), -1), (dict(table=None), -1), (dict(len=None), -1), (dict(refs=DUMMY + 2), -3), (dict(len=DUMMY + 1), -3)]
 BAD_HEADS = [(dict(Hkv=3), -2), (dict(hd=260), -2), (dict(hd=12), -2), (dict(hd=0), -1), (dict(Hq=0), -1), (dict(Hkv=0), -1), (dict(dtype=2), -1)]
 
@@ -608,9 +609,11 @@ def test_tree_attention_refuses():
         assert _attend(**kw) == want, kw
     for kw, want in [(dict(k=None), -1), (dict(v=None), -1), (dict(k=DUMMY + 8), -3), (dict(v=DUMMY + 8), -3)]:
         assert _attend(layer=_layer(**kw)) == want, kw
-    assert sp.lib.spiffy_tree_attention_workspace_bytes(C.byref(_heads()), C.byref(_host()), 5, 5) > 0
-    for T, m in ((0, 1), (1, 0), (1, 1025), ((1 << 20) + 1, 1)):
-        assert sp.lib.spiffy_tree_attention_workspace_bytes(C.byref(_heads()), C.byref(_host()), T, m) == 0
+    size = lambda m, **kw: sp.lib.spiffy_tree_attention_workspace_bytes(C.byref(_heads()), C.byref(_host(**kw)), m)
+    assert size(5) > 0 and size(0) == 0 and size(1025) == 0 and size(5, n_pages=0) == 0
+    many = _heads(Hq=4096, Hkv=4096, hd=8)
+    assert _attend(cfg=many, cache=_host(n_seqs=4096), qs=32768, ks=32768, os=32768) == -2
+    assert sp.lib.spiffy_tree_attention_workspace_bytes(C.byref(many), C.byref(_host(n_seqs=4096)), 5) == 0
 
 
 def _select(cfg=None, cache=None, layer=None, **kw):
