@@ -14,15 +14,14 @@
 // the number of units that fill the GPU, so a long sequence beside short ones is spread over all of it.  The four wavefronts
 // of a unit take steps of 32 (fp32: 16) keys in turn, each with its own running maximum and sum; they are joined in LDS, and units of one
 // sequence by a second kernel, always in the same order.
-#include "paged.h"
+#include "paged_attn.h"
 
 namespace spiffy {
 
 namespace {
 
-constexpr int kAlign = 128;             // keys: unit borders, four wavefronts' steps
-constexpr int kMinChunk = 256;          // keys of a unit at least
 constexpr int kTargetGroups = 1024;     // workgroups that the units of a call are to make
+constexpr int kWideGroups = 256;        // ... of the wide kernel, one a CU
 constexpr int kEntries = 1026;          // pages that are looked up at a time
 constexpr int kBatch = 1024;            // ... by keys: pages of one row, and
 constexpr int kBatchFast = 16384;       // pages of 16 rows, from an entry's middle to another's
@@ -34,97 +33,31 @@ template <> struct Vec<bf16_t> { typedef bf16x8 k; typedef bf16x8 v8; typedef bf
 template <typename T, int N> struct ValueVec { typedef typename Vec<T>::v8 type; };
 template <> struct ValueVec<bf16_t, 4> { typedef bf16x4 type; };
 
-__device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-__device__ __forceinline__ bool finite_bits(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80u) != 0x7f80u; }
-
-// Weight of a partial result whose maximum is m in one whose maximum is top (logarithms to base 2)
-__device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : __builtin_amdgcn_exp2f(m - top); }
-
-struct Unit {
-  int s, index, units, slot;            // slot of the sequence's first partial result
-  long long chunk;
-  RowRange rows;
-  int eff, tree0, total;                // keys of the cache, number of the first new row, end of the numbering
-};
-
-__device__ __forceinline__ void measure(const TreeAttnArgs& a, int s, Unit& u) {
-  u.rows = rows_of(a.rows, s);
-  if (u.rows.n > a.max_rows) u.rows.n = a.max_rows;
-  // below 2^31 - 2^16 (checked on the host), so that numbers of new rows and of batches fit behind it
-  u.eff = a.selected ? a.n_sel * a.c.page_size : seq_len(a.c, s);
-  u.tree0 = (u.eff + kAlign - 1) / kAlign * kAlign;
-  u.total = u.tree0 + u.rows.n;
+// Wavefronts a SIMD that the registers are to leave room for: accumulators, and keys and values in flight, beside some 60 others
+constexpr int waves_of(int hdp, int rt) {
+  const int regs = rt * hdp / 4 + hdp / 2;
+  return regs <= 64 ? 3 : (regs <= 128 ? 2 : 1);
 }
-__device__ __forceinline__ int units_of(int total, long long chunk) {
-  const int n = (int)((total + chunk / 2) / chunk);
-  return n < 1 ? 1 : n;
-}
-
-// The unit of number `id`, found by every thread of the workgroup; s < 0 if there are fewer.
-__device__ Unit find_unit(const TreeAttnArgs& a, int id, int want) {
-  __shared__ long long sums[4];
-  __shared__ int tmp[4], found[3];
-  const int tid = threadIdx.x, n_seqs = a.c.n_seqs;
-  Unit u;
-  long long keys = 0;
-  for (int s = tid; s < n_seqs; s += 256) {
-    measure(a, s, u);
-    if (u.rows.n > 0) keys += u.total;
-  }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) keys += __shfl_xor(keys, o, kWave);
-  if ((tid & 63) == 0) sums[tid >> 6] = keys;
-  if (tid == 0) found[0] = -1;
-  __syncthreads();
-  keys = sums[0] + sums[1] + sums[2] + sums[3];
-  long long chunk = (keys + want - 1) / want;
-  chunk = (chunk + kAlign - 1) / kAlign * kAlign;
-  if (chunk < kMinChunk) chunk = kMinChunk;
-  int before = 0, slots = 0;
-  for (int b = 0; b < n_seqs; b += 256) {
-    const int s = b + tid;
-    int n = 0;
-    if (s < n_seqs) {
-      measure(a, s, u);
-      n = u.rows.n > 0 ? units_of(u.total, chunk) : 0;
-    }
-    int all, all_slots;
-    const int at = before + block_scan(n, tmp, all), slot = slots + block_scan(n > 1 ? n : 0, tmp, all_slots);
-    if (id >= at && id < at + n) found[0] = s, found[1] = at, found[2] = slot;
-    before += all;
-    slots += all_slots;
-  }
-  __syncthreads();
-  u.s = found[0];
-  if (u.s < 0) return u;
-  measure(a, u.s, u);
-  u.index = id - found[1];
-  u.units = units_of(u.total, chunk);
-  u.slot = found[2];
-  u.chunk = chunk;
-  return u;
-}
-
-struct AttnWs {
-  int2* plan;       // [n_seqs]: units of a sequence, slot of its first partial result
-  float2* ml;       // [slots][Hkv][rows]: maximum (base 2) and sum
-  float* o;         // [slots][Hkv][rows][hd]
-  int rows;         // rows of a (slot, kv head)
-};
 
 // FAST: head_dim == HDP, pages of a power of two rows, 16 at least: a 16-key tile lies in one page.  Otherwise every lane looks its
 // rows up, and channels from head_dim on count as zero.
 template <typename T, int HDP, int RT, bool FAST>
-__global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, const AttnWs ws, int want, int row_tiles, int log_ps) {
+__global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const TreeAttnArgs a, const AttnWs ws, int want,
+                                                                                      int row_tiles, int log_ps) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NT = BF ? 2 : 1;                          // 16-key tiles of a step
   constexpr int KW = 16 / sizeof(T), NC = HDP / (4 * KW); // channels of a lane's piece of a key, pieces
   constexpr int VW = HDP / 16 < KW ? HDP / 16 : KW, NP = HDP / (16 * VW);
   constexpr int STEP = 16 * NT;
   constexpr int LD = HDP + 4;                             // row stride of the join buffer: 16 rows in 16 different bank groups
+  constexpr bool QLDS = RT > 1;                           // queries stay in LDS: registers for a second wavefront a SIMD
   typedef typename Vec<T>::k kvec_t;
   typedef typename ValueVec<T, VW>::type vvec_t;
-  extern __shared__ __align__(16) unsigned char smem[];
+  // probabilities as the second product takes them: bf16 of eight keys, fp32 of four
+  typedef typename Vec<T>::k pvec_t;
+  __shared__ __align__(16) float join[4][16][LD];
+  __shared__ __align__(16) kvec_t s_q[QLDS ? RT * NC * kWave : 1];
+  __shared__ uint64_t bits[kMaxWords * RT * 16];          // [words][RT * 16]
   __shared__ int page_id[kEntries], page_rows[kEntries];
   __shared__ float s_m[4][RT * 16], s_l[4][RT * 16];
   const PagedView& c = a.c;
@@ -140,10 +73,29 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
   if (r0 >= R) return;
   const int lo = (int)(u.index * u.chunk), hi = u.index == u.units - 1 ? u.total : lo + (int)u.chunk;
 
+  // The scale is taken as positive; its sign goes to the queries, and a scale of zero makes them zero.
+  const float sign = a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f);
+  const float scale = sign == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;
+  auto load_query = [&](int t, int i) {
+    const int r = min(r0 + t * 16 + l16, R - 1), ch = i * 4 * KW + grp * KW;
+    const T* p = reinterpret_cast<const T*>(a.q) + (u.rows.first + r / g) * a.q_stride + (kvh * g + r % g) * hd;
+    kvec_t x = FAST || ch < hd ? *reinterpret_cast<const kvec_t*>(p + ch) : kvec_t{};
+    if (sign != 1.f)
+#pragma unroll
+      for (int e = 0; e < KW; ++e) x[e] = (T)((float)x[e] * sign);
+    return x;
+  };
+  kvec_t q[QLDS ? 1 : NC];
+  if constexpr (QLDS) {
+    for (int i = wave; i < RT * NC; i += 4) s_q[i * kWave + lane] = load_query(i / NC, i % NC);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) q[i] = load_query(0, i);
+  }
+
   // the tree's bits of this workgroup's rows
-  uint64_t* bits = reinterpret_cast<uint64_t*>(smem);     // [words][RT * 16], in front of the join buffer's use
-  const int words = (u.rows.n + 63) >> 6;
   if (hi > u.tree0) {
+    const int words = (u.rows.n + 63) >> 6;
     for (int i = tid; i < words * RT * 16; i += 256) {
       const int r = i % (RT * 16), w = i / (RT * 16);
       const int row = r0 + r < R ? (r0 + r) / g : 0, left = u.rows.n - 64 * w;
@@ -153,18 +105,6 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
     }
   }
 
-  kvec_t q[RT][NC];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int r = min(r0 + t * 16 + l16, R - 1);
-    const T* p = reinterpret_cast<const T*>(a.q) + (u.rows.first + r / g) * a.q_stride + (kvh * g + r % g) * hd;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int ch = i * 4 * KW + grp * KW;
-      q[t][i] = FAST || ch < hd ? *reinterpret_cast<const kvec_t*>(p + ch) : kvec_t{};
-    }
-  }
-  const float scale = a.scale * 1.4426950408889634f;
   float m[RT], l[RT];
   f32x4 o[RT][NP][VW];
 #pragma unroll
@@ -179,11 +119,11 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
 
   kvec_t k[NT][NC];
   vvec_t v[4 * NT][NP];
-  auto load_key = [&](const T* row, int t) {
+  auto load_key = [&](const T* row, int n) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int ch = i * 4 * KW + grp * KW;
-      k[t][i] = FAST || ch < hd ? *reinterpret_cast<const kvec_t*>(row + ch) : kvec_t{};
+      k[n][i] = FAST || ch < hd ? *reinterpret_cast<const kvec_t*>(row + ch) : kvec_t{};
     }
   };
   auto load_value = [&](const T* row, int j) {
@@ -193,33 +133,35 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
       v[j][p] = FAST || ch < hd ? *reinterpret_cast<const vvec_t*>(row + ch) : vvec_t{};
     }
   };
-  auto scores = [&](int t, f32x4* s) {                    // row tile t against the step's keys
+  // Row tile t against the step's keys, not yet scaled
+  auto scores = [&](int t, f32x4* s) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NT; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
+    for (int i = 0; i < NC; ++i) {
+      const kvec_t x = QLDS ? s_q[(t * NC + i) * kWave + lane] : q[QLDS ? 0 : i];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
         if constexpr (BF) {
-          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n][i], q[t][i], x, 0, 0, 0);
+          s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[n][i], x, s[n], 0, 0, 0);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(k[n][i][e], q[t][i][e], x, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[n][i][e], x[e], s[n], 0, 0, 0);
         }
       }
-      s[n] = x * scale;
     }
   };
-  // Running maximum and sum; s becomes the probabilities.  A column is rescaled only when a score passes its maximum in use by 2^8: with
-  // a maximum that is too low by less all is as exact, probabilities are just up to 256 instead of 1.  No column's arithmetic depends on
-  // another's.
-  auto soften = [&](int t, f32x4* s) {
+  // Running maximum and sum; returns the probabilities.  A column is rescaled only when a score passes its maximum in use by 2^8: with a
+  // maximum that is too low by less all is as exact, probabilities are just up to 256 instead of 1.  No column's arithmetic depends
+  // on another's.  In bf16 a probability is rounded by up to 2^-8 of itself, as the stored values are; their sum is not.
+  auto soften = [&](int t, const f32x4* s) {
     float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][i]);
     auto larger = [](float x, float y) { return fmaxf(x, y); };
-    top = reduce_16(reduce_32(top, larger), larger);
+    top = reduce_16(reduce_32(top, larger), larger) * scale;
     if (__any(top > m[t] + 8.f)) {
       const float m2 = top > m[t] + 8.f ? top : m[t], f = weight(m[t], m2);
       m[t] = m2;
@@ -230,34 +172,37 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
         for (int e = 0; e < VW; ++e) o[t][p][e] *= f;
     }
     const float base = m[t] == -INFINITY ? 0.f : m[t];    // no score so far: every difference is minus infinity
+    pvec_t x;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[n][i] = __builtin_amdgcn_exp2f(s[n][i] - base);
-        l[t] += s[n][i];
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], scale, -base));
+        l[t] += p;
+        x[4 * n + i] = (T)p;
       }
+    return x;
   };
-  auto multiply = [&](const f32x4* s, auto value, f32x4 acc) {      // value(j): of this lane's j-th key
+  auto multiply = [&](pvec_t w, pvec_t x, f32x4 acc) {    // w: one channel of this lane's keys
     if constexpr (BF) {
-      bf16x8 w, x;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        w[j] = value(j);
-        x[j] = static_cast<bf16_t>(s[j >> 2][j & 3]);     // rounded to bf16: off by 2^-8 of itself at most, as the stored values are
-      }
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(value(j), s[0][j], acc, 0, 0, 0);
+      for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w[j], x[j], acc, 0, 0, 0);
       return acc;
     }
   };
-  auto add_values = [&](int t, const f32x4* s) {
+  auto add_values = [&](const pvec_t* x) {                // all row tiles: a channel's operand is put together once
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int e = 0; e < VW; ++e) o[t][p][e] = multiply(s, [&](int j) { return (T)v[j][p][e]; }, o[t][p][e]);
+      for (int e = 0; e < VW; ++e) {
+        pvec_t w;
+#pragma unroll
+        for (int j = 0; j < 4 * NT; ++j) w[j] = (T)v[j][p][e];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) o[t][p][e] = multiply(w, x[t], o[t][p][e]);
+      }
   };
 
   // ---- the cache
@@ -270,45 +215,50 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
     const int end = min(cache_hi, batch + BATCH);
     const int e0 = FAST ? batch >> log_ps : batch / ps, e1 = FAST ? (end - 1) >> log_ps : (end - 1) / ps;
     __syncthreads();
+    const int len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += 256) {
       const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
       int id = -1, rows = 0;
       if (slot >= 0 && slot < c.max_pages) {
         id = c.table[(long long)u.s * c.max_pages + slot];
-        rows = id >= 0 && id < c.n_pages ? clamp_int(seq_len(c, u.s) - slot * ps, 0, ps) : 0;
+        rows = id >= 0 && id < c.n_pages ? clamp_int(len - slot * ps, 0, ps) : 0;
       }
       page_id[e - e0] = rows ? id : 0;
       page_rows[e - e0] = rows;
     }
     __syncthreads();
-    for (int at = batch + wave * STEP; at < end; at += 4 * STEP) {
-      if constexpr (FAST) {
-        int have[NT];
-        const T *kb[NT], *vb[NT];
+    if constexpr (FAST) {
+      int have[NT];                                       // rows of the tiles; they and where the tiles lie are the same in all lanes
+      long long where[NT];
+      auto find = [&](int& at) {                          // the first step from `at` on that has rows
+        for (; at < end; at += 4 * STEP) {
+          bool some = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int key = at + 16 * n, e = __builtin_amdgcn_readfirstlane((min(key, end - 1) >> log_ps) - e0), off = key & (ps - 1);
-          const int page = __builtin_amdgcn_readfirstlane(page_id[e]), rows = __builtin_amdgcn_readfirstlane(page_rows[e]);
-          have[n] = key < end ? min(rows - off, 16) : 0;
-          const long long r = page * row_of_page + (long long)kvh * ps + (key < end ? off : 0);
-          kb[n] = pk + r * HDP;
-          vb[n] = pv + r * HDP;
+          for (int n = 0; n < NT; ++n) {
+            const int key = at + 16 * n, e = (min(key, end - 1) >> log_ps) - e0, off = key & (ps - 1);
+            const int page = __builtin_amdgcn_readfirstlane(page_id[e]), rows = __builtin_amdgcn_readfirstlane(page_rows[e]);
+            have[n] = key < end ? min(rows - off, 16) : 0;
+            where[n] = (page * row_of_page + (long long)kvh * ps + (have[n] > 0 ? off : 0)) * HDP;
+            some |= have[n] > 0;
+          }
+          if (some) break;
         }
-        if (have[0] <= 0 && have[NT - 1] <= 0) continue;
+      };
+      int at = batch + __builtin_amdgcn_readfirstlane(wave) * STEP;
+      find(at);
+      if (at < end)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) load_key(kb[n] + l16 * HDP, n);
+        for (int n = 0; n < NT; ++n) load_key(pk + where[n] + l16 * HDP, n);
+      while (at < end) {
+        // values are in flight during the scores, the next step's keys during the second product
 #pragma unroll
-        for (int j = 0; j < 4 * NT; ++j) load_value(vb[j >> 2] + (4 * grp + (j & 3)) * HDP, j);
-        const bool whole = have[0] == 16 && have[NT - 1] == 16;
-        if (!whole) {                                     // rows behind the last one may hold anything
+        for (int j = 0; j < 4 * NT; ++j) load_value(pv + where[j >> 2] + (4 * grp + (j & 3)) * HDP, j);
+        int had[NT];
+        bool whole = true;
 #pragma unroll
-          for (int j = 0; j < 4 * NT; ++j)
-            if (4 * grp + (j & 3) >= have[j >> 2])
-#pragma unroll
-              for (int p = 0; p < NP; ++p) v[j][p] = vvec_t{};
-        }
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
+        for (int n = 0; n < NT; ++n) had[n] = have[n], whole &= have[n] == 16;
+        pvec_t x[RT];
+        auto weigh = [&](int t) {
           f32x4 s[NT];
           scores(t, s);
           if (!whole) {
@@ -316,12 +266,28 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
             for (int n = 0; n < NT; ++n)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                if (4 * grp + i >= have[n]) s[n][i] = -INFINITY;
+                if (4 * grp + i >= had[n]) s[n][i] = -INFINITY;
           }
-          soften(t, s);
-          add_values(t, s);
+          x[t] = soften(t, s);
+        };
+#pragma unroll
+        for (int t = 0; t < RT; ++t) weigh(t);
+        at += 4 * STEP;
+        find(at);
+        if (at < end)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) load_key(pk + where[n] + l16 * HDP, n);
+        if (!whole) {                                     // rows behind the last one may hold anything
+#pragma unroll
+          for (int j = 0; j < 4 * NT; ++j)
+            if (4 * grp + (j & 3) >= had[j >> 2])
+#pragma unroll
+              for (int p = 0; p < NP; ++p) v[j][p] = vvec_t{};
         }
-      } else {
+        add_values(x);
+      }
+    } else {
+      for (int at = batch + wave * STEP; at < end; at += 4 * STEP) {
         auto row_of = [&](int key, bool& there) {         // row of the pool; row 0 where there is none
           const int kk = min(key, end - 1), e = kk / ps, off = kk - e * ps;
           there = key < end && off < page_rows[e - e0];
@@ -337,6 +303,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
 #pragma unroll
             for (int p = 0; p < NP; ++p) v[j][p] = vvec_t{};
         }
+        pvec_t x[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           f32x4 s[NT];
@@ -346,9 +313,9 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (!there[n][i]) s[n][i] = -INFINITY;
-          soften(t, s);
-          add_values(t, s);
+          x[t] = soften(t, s);
         }
+        add_values(x);
       }
     }
   }
@@ -383,10 +350,9 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
         }
       }
     }
-    const bool some_odd = __any(odd != 0);
+    pvec_t x[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      if (!__any(seen[t] != 0)) continue;
       f32x4 s[NT];
       scores(t, s);
 #pragma unroll
@@ -394,25 +360,31 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (!(seen[t] >> (16 * n + 4 * grp + i) & 1)) s[n][i] = -INFINITY;
-      soften(t, s);
-      add_values(t, s);
-      // Zero times NaN is NaN: a value that is not finite is added key by key, only in the columns that attend to the key.
-      if (some_odd) {
+      x[t] = soften(t, s);
+    }
+    add_values(x);
+    // Zero times NaN is NaN: a value that is not finite is added key by key, only in the columns that attend to the key.
+    if (__any(odd != 0)) {
 #pragma unroll 1
-        for (int x = 0; x < STEP; ++x) {
-          const int owner = x >> 2 & 3, slot = (x >> 4) * 4 + (x & 3);
-          if (!__any(grp == owner && (odd >> slot & 1))) continue;
-          const T* row = reinterpret_cast<const T*>(a.v) + (first + min(at + x, u.rows.n - 1)) * a.kv_stride + kvh * hd;
-          const bool mine = seen[t] >> x & 1;
+      for (int y = 0; y < STEP; ++y) {
+        const int owner = y >> 2 & 3, slot = (y >> 4) * 4 + (y & 3);
+        if (!__any(grp == owner && (odd >> slot & 1))) continue;
+        const T* row = reinterpret_cast<const T*>(a.v) + (first + min(at + y, u.rows.n - 1)) * a.kv_stride + kvh * hd;
 #pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const int ch = p * 16 * VW + l16 * VW;
-            const vvec_t w = grp == owner && (FAST || ch < hd) ? *reinterpret_cast<const vvec_t*>(row + ch) : vvec_t{};
+        for (int p = 0; p < NP; ++p) {
+          const int ch = p * 16 * VW + l16 * VW;
+          const vvec_t z = grp == owner && (FAST || ch < hd) ? *reinterpret_cast<const vvec_t*>(row + ch) : vvec_t{};
 #pragma unroll
-            for (int e = 0; e < VW; ++e) {
-              const f32x4 y = multiply(s, [&](int j) { return j != slot || finite_bits((T)w[e]) ? (T)0.f : (T)w[e]; }, f32x4{0.f, 0.f, 0.f, 0.f});
+          for (int e = 0; e < VW; ++e) {
+            pvec_t w;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[t][p][e][i] = mine ? o[t][p][e][i] + y[i] : o[t][p][e][i];
+            for (int j = 0; j < 4 * NT; ++j) w[j] = j != slot || finite_bits((T)z[e]) ? (T)0.f : (T)z[e];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+              const f32x4 more = multiply(w, x[t], f32x4{0.f, 0.f, 0.f, 0.f});
+              const bool mine = seen[t] >> y & 1;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[t][p][e][i] = mine ? o[t][p][e][i] + more[i] : o[t][p][e][i];
             }
           }
         }
@@ -420,62 +392,62 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeAttnArgs a, co
     }
   }
 
-  // ---- the four wavefronts' results, joined in their order
+  // ---- the four wavefronts' results, joined in their order, a row tile at a time
   auto plus = [](float x, float y) { return x + y; };
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const float sum = reduce_16(reduce_32(l[t], plus), plus);
     if (grp == 0) s_m[wave][t * 16 + l16] = m[t], s_l[wave][t * 16 + l16] = sum;
   }
-  __syncthreads();                                        // also behind the last use of `bits`
-  float* join = reinterpret_cast<float*>(smem);           // [4][RT * 16][LD]
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int r = t * 16 + l16;
-    const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r])), f = weight(m[t], top);
-    float* to = join + (wave * RT * 16 + r) * LD;
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < VW; e += 4)
-          *reinterpret_cast<f32x4*>(to + p * 16 * VW + (4 * grp + i) * VW + e) =
-              f32x4{o[t][p][e][i], o[t][p][e + 1][i], o[t][p][e + 2][i], o[t][p][e + 3][i]} * f;
-  }
   __syncthreads();
   const long long part = ((long long)(u.slot + u.index) * a.h.Hkv + kvh) * ws.rows + r0;
-  for (int x = tid; x < RT * 16 * (HDP / 4); x += 256) {
-    const int r = x / (HDP / 4), ch = x % (HDP / 4) * 4;
-    if (r0 + r >= R || ch >= hd) continue;
-    const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
-    float sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      sum += s_l[w][r] * weight(s_m[w][r], top);
-      y += *reinterpret_cast<const f32x4*>(join + (w * RT * 16 + r) * LD + ch);
+  for (int t = 0; t < RT; ++t) {
+    if (r0 + t * 16 >= R) break;
+    {
+      const int r = t * 16 + l16;
+      const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r])), f = weight(m[t], top);
+      float* to = join[wave][l16];
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < VW; e += 4)
+            *reinterpret_cast<f32x4*>(to + p * 16 * VW + (4 * grp + i) * VW + e) =
+                f32x4{o[t][p][e][i], o[t][p][e + 1][i], o[t][p][e + 2][i], o[t][p][e + 3][i]} * f;
     }
-    if (u.units > 1) {
-      *reinterpret_cast<f32x4*>(ws.o + (part + r) * hd + ch) = y;
-      if (ch == 0) ws.ml[part + r] = make_float2(top, sum);
-    } else {
-      T* out = reinterpret_cast<T*>(a.out) + (u.rows.first + (r0 + r) / g) * a.out_stride + (kvh * g + (r0 + r) % g) * hd + ch;
-      const float f = sum == 0.f ? 0.f : 1.f / sum;
-      typedef T out4 __attribute__((ext_vector_type(4)));
-      *reinterpret_cast<out4*>(out) = out4{from_f32<T>(sum == 0.f ? 0.f : y[0] * f), from_f32<T>(sum == 0.f ? 0.f : y[1] * f),
-                                           from_f32<T>(sum == 0.f ? 0.f : y[2] * f), from_f32<T>(sum == 0.f ? 0.f : y[3] * f)};
+    __syncthreads();
+    for (int y = tid; y < 16 * (HDP / 4); y += 256) {
+      const int rr = y / (HDP / 4), r = t * 16 + rr, ch = y % (HDP / 4) * 4;
+      if (r0 + r >= R || ch >= hd) continue;
+      const float top = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+      float sum = 0.f;
+      f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        sum += s_l[w][r] * weight(s_m[w][r], top);
+        z += *reinterpret_cast<const f32x4*>(join[w][rr] + ch);
+      }
+      if (u.units > 1) {
+        *reinterpret_cast<f32x4*>(ws.o + (part + r) * hd + ch) = z;
+        if (ch == 0) ws.ml[part + r] = make_float2(top, sum);
+      } else {
+        T* out = reinterpret_cast<T*>(a.out) + (u.rows.first + (r0 + r) / g) * a.out_stride + (kvh * g + (r0 + r) % g) * hd + ch;
+        store_row(out, z, sum);
+      }
     }
+    if (t + 1 < RT) __syncthreads();
   }
 }
 
-// One workgroup a (new row, query head): the partial results of its sequence's units, in order.
+// One workgroup (of one wavefront or four) a (new row, query head): the partial results of its sequence's units, in order.
 template <typename T>
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeAttnArgs a, const AttnWs ws) {
   __shared__ float s_top[4];
   __shared__ __align__(16) f32x4 s_o[256];
   __shared__ float s_l[256];
-  const int tid = threadIdx.x, t = blockIdx.x, h = blockIdx.y, g = a.h.Hq / a.h.Hkv, kvh = h / g, hd = a.h.hd;
+  const int tid = threadIdx.x, n = blockDim.x, t = blockIdx.x, h = blockIdx.y, g = a.h.Hq / a.h.Hkv, kvh = h / g, hd = a.h.hd;
   const int s = seq_of_row(a.rows, a.c.n_seqs, t);
   if (s >= a.c.n_seqs) return;
   const RowRange r = rows_of(a.rows, s);
@@ -485,12 +457,14 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeAttnArgs a, co
   if (plan.x <= 1) return;
   const long long step = (long long)a.h.Hkv * ws.rows, first = plan.y * step + (long long)kvh * ws.rows + row * g + (h - kvh * g);
   float top = -INFINITY;
-  for (int i = tid; i < plan.x; i += 256) top = fmaxf(top, ws.ml[first + i * step].x);
+  for (int i = tid; i < plan.x; i += n) top = fmaxf(top, ws.ml[first + i * step].x);
   top = wave_max(top);
-  if ((tid & 63) == 0) s_top[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-  const int pieces = hd / 4, groups = 256 / pieces, grp = tid / pieces, pc = tid - grp * pieces;
+  if (n > kWave) {
+    if ((tid & 63) == 0) s_top[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  }
+  const int pieces = hd / 4, groups = n / pieces, grp = tid / pieces, pc = tid - grp * pieces;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f;
   if (grp < groups) {
@@ -510,10 +484,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeAttnArgs a, co
     o += s_o[i * pieces + pc];
     l += s_l[i * pieces + pc];
   }
-  T* out = reinterpret_cast<T*>(a.out) + t * a.out_stride + h * hd + pc * 4;
-  typedef T out4 __attribute__((ext_vector_type(4)));
-  const float f = 1.f / l;
-  *reinterpret_cast<out4*>(out) = l == 0.f ? out4{} : out4{from_f32<T>(o[0] * f), from_f32<T>(o[1] * f), from_f32<T>(o[2] * f), from_f32<T>(o[3] * f)};
+  store_row(reinterpret_cast<T*>(a.out) + t * a.out_stride + h * hd + pc * 4, o, l);
 }
 
 // Row tiles of a workgroup: enough for all rows of a (sequence, kv head), 64 at most (fp32: 32; more than 128 channels: 16; registers)
@@ -524,15 +495,17 @@ int row_tiles_of(const Heads& h, int max_rows) {
   return need < most ? need : most;
 }
 struct Shape {
+  int wide;                 // 0: the kernel of this file, else the halves of csrc/paged_attn_wide.hip
   int rt, tiles, want, rows;
   long long slots;
 };
 Shape shape_of(const Heads& h, int max_rows) {
   Shape s;
-  s.rt = row_tiles_of(h, max_rows);
   s.rows = max_rows * (h.Hq / h.Hkv);
-  s.tiles = cdiv(s.rows, 16 * s.rt);
-  s.want = kTargetGroups / (h.Hkv * s.tiles);
+  s.wide = h.f32 || h.hd > 128 || s.rows <= 64 ? 0 : (s.rows <= 128 ? 2 : 1);
+  s.rt = row_tiles_of(h, max_rows);
+  s.tiles = cdiv(s.rows, s.wide ? wide_rows(s.wide) : 16 * s.rt);
+  s.want = (s.wide ? kWideGroups : kTargetGroups) / (h.Hkv * s.tiles);
   if (s.want < 1) s.want = 1;
   // a sequence of two units or more has at least 1.5 chunks, so its units are at most 4/3 of its keys over the chunk
   s.slots = 4ll * s.want / 3 + 2;
@@ -543,16 +516,8 @@ size_t ml_bytes(const Heads& h, const Shape& s) { return align_up(sizeof(float2)
 
 template <typename T, int HDP, int RT, bool FAST>
 hipError_t launch_one(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, int log_ps, hipStream_t st) {
-  constexpr int kLds = 4 * RT * 16 * (HDP + 4) * (int)sizeof(float);
-  constexpr int kBits = kMaxWords * RT * 16 * (int)sizeof(uint64_t);
-  constexpr int lds = kLds > kBits ? kLds : kBits;
-  static std::atomic<unsigned long long> done{0};
-  if (lds > 64 * 1024 - 12 * 1024) {
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&tree_attn_kernel<T, HDP, RT, FAST>), lds, done);
-    if (e != hipSuccess) return e;
-  }
   const long long grid = ((long long)s.want + a.c.n_seqs) * a.h.Hkv * s.tiles;
-  tree_attn_kernel<T, HDP, RT, FAST><<<(unsigned)grid, 256, lds, st>>>(a, ws, s.want, s.tiles, log_ps);
+  tree_attn_kernel<T, HDP, RT, FAST><<<(unsigned)grid, 256, 0, st>>>(a, ws, s.want, s.tiles, log_ps);
   return hipGetLastError();
 }
 template <typename T, int HDP, int RT>
@@ -591,15 +556,18 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   ws.o = reinterpret_cast<float*>(p + plan_bytes(a.c) + ml_bytes(a.h, s));
   ws.rows = s.rows;
   hipError_t e;
-  if (a.h.f32) e = a.h.hd <= 64 ? launch_rows<float, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<float, 128>(a, ws, s, st) : launch_rows<float, 256>(a, ws, s, st);
+  if (s.wide) e = launch_tree_wide(a, ws, s.want, s.tiles, s.wide, st);
+  else if (a.h.f32) e = a.h.hd <= 64 ? launch_rows<float, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<float, 128>(a, ws, s, st) : launch_rows<float, 256>(a, ws, s, st);
   else e = a.h.hd <= 64 ? launch_rows<bf16_t, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<bf16_t, 128>(a, ws, s, st) : launch_rows<bf16_t, 256>(a, ws, s, st);
   if (e != hipSuccess) return e;
   // no sequence can have more than one unit: nothing to join
   const long long most = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size + kAlign + a.max_rows;
   if (2 * most < 3 * kMinChunk) return hipSuccess;
+  // few rows have many partial results each and wait for them: four wavefronts a row; many rows: one
   const dim3 grid(a.rows.T, a.h.Hq);
-  if (a.h.f32) tree_join_kernel<float><<<grid, 256, 0, st>>>(a, ws);
-  else tree_join_kernel<bf16_t><<<grid, 256, 0, st>>>(a, ws);
+  const int threads = (long long)a.rows.T * a.h.Hq <= 2048 ? 256 : 64;
+  if (a.h.f32) tree_join_kernel<float><<<grid, threads, 0, st>>>(a, ws);
+  else tree_join_kernel<bf16_t><<<grid, threads, 0, st>>>(a, ws);
   return hipGetLastError();
 }
 

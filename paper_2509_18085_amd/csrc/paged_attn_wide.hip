@@ -1,0 +1,371 @@
+// Attention of drafted token trees over a paged cache, many rows a kv head (bf16, head_dim up to 128).
+//
+// With more than 64 rows the matrix instructions are the bound, and a key has to serve them all: eight wavefronts of 32 rows each share
+// tiles of 64 keys through LDS.  HALVES == 1: 256 rows, a wavefront takes all of a tile; HALVES == 2: 128 rows, wavefronts w and w + 4
+// have the same rows and a half of every tile each, joined at the end.
+//
+// S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions.  Accumulator element x of lane (column l32 = lane % 32, half = lane / 32) is
+// key 8 (x / 4) + 4 half + x % 4, so elements 8 i .. 8 i + 7 are the second product's operand of its i-th step as they stand, with V's
+// rows taken in that order by the transposing LDS read (four rows a lane).  Rows lie in LDS as in memory, their 16-byte
+// pieces permuted so that neither kind of read meets a bank twice.
+//
+// Tile t's second product runs against tile t + 1's first: keys are one tile ahead of values in LDS, two tiles ahead of the arithmetic in
+// registers, with one barrier a tile.
+#include "paged_attn.h"
+
+namespace spiffy {
+
+namespace {
+
+constexpr int kThreads = 512, kTile = 64;
+constexpr int kWideEntries = 4098;                        // pages that are looked up at a time ...
+constexpr int kWideKeys = 65536;                          // ... for so many keys at most
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4_ptr_t;
+
+template <int HDP, int HALVES>
+__global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnArgs a, const AttnWs ws, int want, int row_tiles, int log_ps) {
+  constexpr int ROWS = wide_rows(HALVES);
+  constexpr int SUB = 2 / HALVES;                         // 32-key tiles of a wavefront
+  constexpr int NK = HDP / 16, NN = HDP / 32;             // steps of the first product, 32-channel tiles of the second
+  constexpr int PIECES = HDP / 8, RPT = kTile * PIECES / kThreads;      // 16-byte pieces of a row; rows of a thread
+  constexpr int RSTEP = kThreads / PIECES;
+  constexpr int ROWB = HDP * 2, TILEB = kTile * ROWB;
+  // K tiles 0, 1, V tiles 0, 1; before the new rows the page list, behind it their bits
+  __shared__ __align__(16) unsigned char s_kv[4 * TILEB];
+  __shared__ __align__(16) int2 s_page[kWideEntries];     // page, rows in it
+  __shared__ unsigned long long s_any[SPIFFY_MAX_TREE / 64];
+  __shared__ unsigned s_odd[kTile / 32];                  // new rows of a tile whose values are not all finite
+  const PagedView& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int hd = a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
+
+  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int tile = logical % row_tiles, kvh = logical / row_tiles % a.h.Hkv;
+  const Unit u = find_unit(a, logical / row_tiles / a.h.Hkv, want);
+  if (u.s < 0) return;
+  if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
+  const int R = u.rows.n * g, r0 = tile * ROWS;
+  if (r0 >= R) return;
+  const int lo = (int)(u.index * u.chunk), hi = u.index == u.units - 1 ? u.total : lo + (int)u.chunk;
+  const int group = HALVES == 2 ? wave & 3 : wave, part = HALVES == 2 ? wave >> 2 : 0;
+  const int row = r0 + group * 32 + l32;                  // this lane's column
+  const bool busy = r0 + group * 32 < R;                  // the same for the wavefront: it has rows
+
+  const float sign = a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f);
+  const float scale = sign == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;
+  bf16x8 q[NK];
+  {
+    const int r = min(row, R - 1);
+    const bf16_t* p = reinterpret_cast<const bf16_t*>(a.q) + (u.rows.first + r / g) * a.q_stride + (kvh * g + r % g) * hd;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int ch = 16 * i + 8 * half;
+      q[i] = ch < hd ? *reinterpret_cast<const bf16x8*>(p + ch) : bf16x8{};
+      if (sign != 1.f)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[i][e] = (bf16_t)((float)q[i][e] * sign);
+    }
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[NN];
+#pragma unroll
+  for (int n = 0; n < NN; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
+
+  // ---- LDS: where pieces lie, what a lane reads
+  auto k_at = [](int r, int piece) { return r * ROWB + 16 * (piece ^ (r & (PIECES - 1))); };
+  auto v_at = [](int r, int piece) { return r * ROWB + 16 * (piece ^ ((HDP == 128 ? r & 3 : r >> 1 & 1) << 2)); };
+  auto k_frag = [&](int buf, int sub, int i) {
+    return *reinterpret_cast<const bf16x8*>(s_kv + buf * TILEB + k_at(32 * sub + l32, 2 * i + half));
+  };
+  const unsigned v_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)(s_kv + 2 * TILEB);
+  auto v_frag = [&](int buf, int sub, int i, int n) {     // keys 32 sub + 16 i + 8 e + 4 half .. + 3, channel 32 n + l32
+    bf16x8 x;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 32 * sub + 16 * i + 8 * e + 4 * half + ((lane & 15) >> 2), ch = 32 * n + 16 * (l32 >> 4) + 4 * (lane & 3);
+      const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(size_t)(v_base + buf * TILEB + v_at(r, ch >> 3) + (ch & 7) * 2));
+#pragma unroll
+      for (int z = 0; z < 4; ++z) x[4 * e + z] = y[z];
+    }
+    return x;
+  };
+  auto scores = [&](int buf, f32x16 (&s)[SUB]) {
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, b + part, i), q[i], s[b], 0, 0, 0);
+    }
+  };
+  // keys that this column does not attend to (a bit a key of the tile)
+  auto hide = [&](f32x16 (&s)[SUB], unsigned long long seen) {
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) {
+      const unsigned bits = (unsigned)(seen >> (32 * (b + part))) >> (4 * half);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!(bits >> (8 * (e >> 2) + (e & 3)) & 1)) s[b][e] = -INFINITY;
+    }
+  };
+  // as in the kernel for few rows: a column is rescaled when a score passes the maximum in use by 2^8
+  auto soften = [&](f32x16 (&s)[SUB], bf16x8 (&x)[2 * SUB]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < SUB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+    top = reduce_32(top, [](float p, float r) { return fmaxf(p, r); }) * scale;
+    if (__any(top > m + 8.f)) {
+      const float m2 = top > m + 8.f ? top : m, f = weight(m, m2);
+      m = m2;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < NN; ++n) o[n] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int b = 0; b < SUB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -base));
+        l += p;
+        x[2 * b + (e >> 3)][e & 7] = (bf16_t)p;
+      }
+  };
+  auto add_values = [&](int buf, const bf16x8 (&x)[2 * SUB]) {
+#pragma unroll
+    for (int b = 0; b < SUB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int n = 0; n < NN; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(buf, b + part, i, n), x[2 * b + i], o[n], 0, 0, 0);
+  };
+
+  // ---- the cache
+  const int my_row = tid / PIECES, my_piece = tid % PIECES;
+  const bf16_t* pk = reinterpret_cast<const bf16_t*>(a.pk);
+  const bf16_t* pv = reinterpret_cast<const bf16_t*>(a.pv);
+  const long long row_of_page = (long long)a.h.Hkv * ps;
+  const int cache_hi = min(hi, u.eff);
+  const int batch_keys = (int)min((long long)(kWideEntries - 2) * ps, (long long)kWideKeys);
+  for (int batch = lo; batch < cache_hi; batch += batch_keys) {
+    const int end = min(cache_hi, batch + batch_keys);
+    auto entry = [&](int key) { return log_ps >= 0 ? key >> log_ps : (int)((unsigned)key / (unsigned)ps); };
+    const int e0 = entry(batch), e1 = entry(end - 1);
+    __syncthreads();
+    const int len = seq_len(c, u.s);
+    for (int e = e0 + tid; e <= e1; e += kThreads) {
+      const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
+      int id = -1, rows = 0;
+      if (slot >= 0 && slot < c.max_pages) {
+        id = c.table[(long long)u.s * c.max_pages + slot];
+        rows = id >= 0 && id < c.n_pages ? clamp_int(len - slot * ps, 0, ps) : 0;
+      }
+      s_page[e - e0] = make_int2(id, rows);
+    }
+    __syncthreads();
+    const int tiles = (end - batch + kTile - 1) / kTile;
+    // row of the pool that holds a key, -1: none
+    auto find = [&](int key) {
+      const int e = entry(min(key, end - 1)), off = min(key, end - 1) - e * ps;
+      const int2 p = s_page[e - e0];
+      return key < end && off < p.y ? p.x * row_of_page + (long long)kvh * ps + off : -1ll;
+    };
+    auto load = [&](const bf16_t* pool, int t, u32x4 (&x)[RPT]) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const long long r = find(batch + t * kTile + my_row + i * RSTEP);
+        x[i] = r >= 0 && my_piece * 8 < hd ? *reinterpret_cast<const u32x4*>(pool + r * hd + my_piece * 8) : u32x4{};
+      }
+    };
+    auto put_keys = [&](int buf, const u32x4 (&x)[RPT]) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + i * RSTEP, my_piece)) = x[i];
+    };
+    auto put_values = [&](int buf, const u32x4 (&x)[RPT]) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + (2 + buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = x[i];
+    };
+    u32x4 kx[RPT], vx[RPT];
+    f32x16 s[SUB], next[SUB];
+    load(pk, 0, kx);
+    load(pv, 0, vx);
+    put_keys(0, kx);
+    put_values(0, vx);
+    if (tiles > 1) {
+      load(pk, 1, kx);
+      put_keys(1, kx);
+    }
+    __syncthreads();
+    if (busy) scores(0, s);
+    for (int t = 0; t < tiles; ++t) {
+      if (t) __syncthreads();                             // keys of tile t + 1 and values of tile t are there, those of t - 1 are done with
+      if (t + 2 < tiles) load(pk, t + 2, kx);
+      if (t + 1 < tiles) load(pv, t + 1, vx);
+      if (busy) {
+        const unsigned long long there = __ballot(find(batch + t * kTile + lane) >= 0);
+        if (there != ~0ull) hide(s, there);
+        bf16x8 x[2 * SUB];
+        if (t + 1 < tiles) scores((t + 1) & 1, next);
+        soften(s, x);
+        add_values(t & 1, x);
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) s[b] = next[b];
+      }
+      if (t + 1 < tiles) put_values((t + 1) & 1, vx);
+      if (t + 2 < tiles) {
+        if (t == 0) __syncthreads();                      // tile 0's keys were read in front of the loop
+        put_keys(t & 1, kx);
+      }
+    }
+  }
+
+  // ---- the new rows
+  if (hi > u.tree0) {
+    uint64_t* bits = reinterpret_cast<uint64_t*>(s_page); // [words][ROWS]
+    static_assert(sizeof(s_page) >= sizeof(uint64_t) * ROWS * (SPIFFY_MAX_TREE / 64), "the bits take the page list's place");
+    const int words = (u.rows.n + 63) >> 6;
+    __syncthreads();
+    if (tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < words * ROWS; i += kThreads) {
+      const int r = i % ROWS, w = i / ROWS, left = u.rows.n - 64 * w;
+      uint64_t b = r0 + r < R ? (left < 64 ? (1ull << left) - 1 : ~0ull) : 0;
+      if (a.rows.mask && b) b &= w < a.rows.words ? a.rows.mask[(long long)(u.rows.first + (r0 + r) / g) * a.rows.words + w] : 0;
+      bits[i] = b;
+      if (b) atomicOr(&s_any[w], (unsigned long long)b);
+    }
+    __syncthreads();
+    const long long first = u.rows.first;
+    for (int at = max(lo - u.tree0, 0); at < hi - u.tree0; at += kTile) {      // whole words: units begin at multiples of 128
+      if (!s_any[at >> 6]) continue;
+      __syncthreads();                                    // the tile before is done with
+      if (tid < kTile / 32) s_odd[tid] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const int r = my_row + i * RSTEP;
+        bf16x8 x = {}, y = {};
+        if (at + r < u.rows.n && my_piece * 8 < hd) {
+          const long long from = (first + at + r) * a.kv_stride + kvh * hd + my_piece * 8;
+          x = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.k) + from);
+          y = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.v) + from);
+        }
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool ok = finite_bits((bf16_t)y[e]);
+          odd |= !ok;
+          y[e] = ok ? (bf16_t)y[e] : (bf16_t)0.f;
+        }
+        if (odd) atomicOr(&s_odd[r >> 5], 1u << (r & 31));
+        *reinterpret_cast<bf16x8*>(s_kv + k_at(r, my_piece)) = x;
+        *reinterpret_cast<bf16x8*>(s_kv + 2 * TILEB + v_at(r, my_piece)) = y;
+      }
+      __syncthreads();
+      const uint64_t seen = bits[(at >> 6) * ROWS + group * 32 + l32];
+      if (__any(seen != 0)) {
+        f32x16 s[SUB];
+        bf16x8 x[2 * SUB];
+        scores(0, s);
+        hide(s, seen);
+        soften(s, x);
+        add_values(0, x);
+        // values that are not finite, key by key, only in the columns that attend to the key
+        for (int b = 0; b < SUB; ++b) {
+          for (unsigned odd = s_odd[b + part]; odd; odd &= odd - 1) {
+            const int y = __ffs(odd) - 1, key = at + 32 * (b + part) + y;      // owner: half (y / 4) % 2, step y / 16, element 4 (y / 8 % 2) + y % 4
+            const bool mine = seen >> (key & 63) & 1;
+            const bf16_t* from = reinterpret_cast<const bf16_t*>(a.v) + (first + key) * a.kv_stride + kvh * hd;
+            const int slot = 4 * (y >> 3 & 1) + (y & 3);
+#pragma unroll
+            for (int n = 0; n < NN; ++n) {
+              const bf16_t z = 32 * n + l32 < hd && half == (y >> 2 & 1) ? from[32 * n + l32] : (bf16_t)0.f;
+              bf16x8 w, p;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                w[j] = j == slot && !finite_bits(z) ? z : (bf16_t)0.f;
+                p[j] = y >> 4 ? (b ? x[2 * SUB - 1][j] : x[1][j]) : (b ? x[2 * SUB - 2][j] : x[0][j]);
+              }
+              f32x16 more;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) more[e] = 0.f;
+              more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p, more, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[n][e] = mine ? o[n][e] + more[e] : o[n][e];
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // ---- results: rows of a lane's column, four channels at a time
+  float sum = reduce_32(l, [](float p, float r) { return p + r; });
+  if constexpr (HALVES == 2) {
+    // The upper halves' results go through LDS, 32 channels at a time.
+    constexpr int LD = 36;
+    static_assert(4 * 32 * LD * sizeof(float) <= sizeof(s_kv) && 4 * 32 * sizeof(float2) <= sizeof(s_page), "join buffers");
+    float* join = reinterpret_cast<float*>(s_kv) + (group * 32 + l32) * LD + 4 * half;
+    float2* stat = reinterpret_cast<float2*>(s_page);
+    __syncthreads();                                      // tiles and bits are done with
+    if (part == 1 && half == 0) stat[group * 32 + l32] = make_float2(m, sum);
+    __syncthreads();
+    const float2 other = stat[group * 32 + l32];
+    const float top = fmaxf(m, other.x), f = weight(m, top), fo = weight(other.x, top);
+#pragma unroll
+    for (int n = 0; n < NN; ++n) {
+      if (part == 1)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) *reinterpret_cast<f32x4*>(join + 2 * e) = f32x4{o[n][e], o[n][e + 1], o[n][e + 2], o[n][e + 3]};
+      __syncthreads();
+      if (part == 0)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const f32x4 z = *reinterpret_cast<const f32x4*>(join + 2 * e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][e + i] = o[n][e + i] * f + z[i] * fo;
+        }
+      __syncthreads();
+    }
+    if (part == 1) return;
+    sum = sum * f + other.y * fo;
+    m = top;
+  }
+  if (row >= R) return;
+  const long long at = ((long long)(u.slot + u.index) * a.h.Hkv + kvh) * ws.rows + row;
+  bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + (u.rows.first + row / g) * a.out_stride + (kvh * g + row % g) * hd;
+  if (u.units > 1 && half == 0) ws.ml[at] = make_float2(m, sum);
+#pragma unroll
+  for (int n = 0; n < NN; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int ch = 32 * n + 2 * e + 4 * half;
+      if (ch >= hd) continue;
+      const f32x4 z = {o[n][e], o[n][e + 1], o[n][e + 2], o[n][e + 3]};
+      if (u.units > 1) *reinterpret_cast<f32x4*>(ws.o + at * hd + ch) = z;
+      else store_row(out + ch, z, sum);
+    }
+}
+
+template <int HDP, int HALVES>
+hipError_t launch_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st) {
+  const int ps = a.c.page_size;
+  const long long grid = ((long long)want + a.c.n_seqs) * a.h.Hkv * row_tiles;
+  tree_wide_kernel<HDP, HALVES><<<(unsigned)grid, kThreads, 0, st>>>(a, ws, want, row_tiles, ps & (ps - 1) ? -1 : __builtin_ctz(ps));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, int halves, hipStream_t st) {
+  if (a.h.hd <= 64) return halves == 2 ? launch_wide<64, 2>(a, ws, want, row_tiles, st) : launch_wide<64, 1>(a, ws, want, row_tiles, st);
+  return halves == 2 ? launch_wide<128, 2>(a, ws, want, row_tiles, st) : launch_wide<128, 1>(a, ws, want, row_tiles, st);
+}
+
+}  // namespace spiffy

@@ -58,6 +58,11 @@ ATTEND = [
     (BF, 2, 2, 8, 1, [70, 3], [3, 1]),
     (BF, 3, 1, 248, 57, [58, 57], [6, 2]),
     (BF, 16, 1, 128, 64, [2000], [1]),
+    (BF, 6, 1, 80, 24, [333, 70, 2], [40, 11, 13]),
+    (BF, 4, 1, 40, 7, [150, 0], [30, 3]),
+    (BF, 2, 1, 64, 5, [3000, 1], [50, 64]),
+    (BF, 2, 2, 128, 16, [5000, 40], [300, 128]),
+    (BF, 16, 1, 128, 1, [900], [8]),
     (F32, 4, 4, 64, 24, [300, 7, 0], [8, 3, 2]),
     (F32, 8, 2, 128, 16, [500, 33], [1, 21]),
     (F32, 4, 1, 128, 64, [129], [70]),
@@ -126,21 +131,21 @@ def test_attention_of_a_block_of_states(dtype, hd, ps):
 @gpu
 @pytest.mark.parametrize("dtype,hd", [(BF, 128), (BF, 64), (F32, 128), (F32, 64), (BF, 40)])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
-def test_what_a_row_does_not_attend_to_does_not_show(dtype, hd, value):
-    """Nodes 3 and 40 hold NaN or infinities; rows that see them get what the formula gives, all others are as if they were not there."""
-    n = 70
+@pytest.mark.parametrize("n,far", [(70, 40), (55, 40), (20, 18), (6, 5)])
+def test_what_a_row_does_not_attend_to_does_not_show(dtype, hd, value, n, far):
+    """Nodes 3 and `far` hold NaN or infinities; rows that see them get what the formula gives, all others are as if they were not there."""
     x = Setup(dtype, 4, 2, hd, 16, [50], [n], seed=4)
-    rows = [r & ~(1 << 3) & ~(1 << 40) if t % 7 else r | 1 << 40 for t, r in enumerate([x.rng.getrandbits(n) for _ in range(n)])]
-    rows[5] = 0
+    rows = [r & ~(1 << 3) & ~(1 << far) if t % 7 else r | 1 << far for t, r in enumerate([x.rng.getrandbits(n) for _ in range(n)])]
+    rows[4] = 0
     base = _on_gpu(x, dtype)
     start = torch.tensor(x.start, dtype=torch.int32, device=DEV)
-    mask = mask_words(rows, 2).to(DEV)
+    mask = mask_words(rows, -(-n // 64)).to(DEV)
     clean = base.attend(0, *x.rows(0, DEV), start, n, mask=mask)
     for part in (4, 6):                       # first kv head's keys, then its values; the second kv head's stay
         x.qkv[0, 3, part] = value
-        x.qkv[0, 40, part, hd // 2] = value
+        x.qkv[0, far, part, hd // 2] = value
     got = base.attend(0, *x.rows(0, DEV), start, n, mask=mask).cpu()
-    blind = [t for t in range(n) if not (rows[t] >> 3 & 1 or rows[t] >> 40 & 1)]
+    blind = [t for t in range(n) if not (rows[t] >> 3 & 1 or rows[t] >> far & 1)]
     assert blind and len(blind) < n
     assert torch.equal(got[blind], clean.cpu()[blind])
     assert torch.equal(got[:, 2:], clean.cpu()[:, 2:])
