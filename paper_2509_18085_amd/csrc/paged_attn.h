@@ -38,9 +38,22 @@ __device__ __forceinline__ long long chunk_of(long long keys, int want) {
   return chunk < kMinChunk ? kMinChunk : chunk;
 }
 
-// The unit of number `id`, found by every thread of the workgroup; s < 0 if there are fewer.  Up to 64 sequences a wavefront finds it
-// by itself, a sequence a lane.
-__device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int id, int want) {
+// A workgroup's part of a call: `per` workgroups (kv heads times row tiles) a unit, those of one unit next to each other on one XCD.  Only
+// the workgroups of units that there are take part in the spread over the XCDs: a launch is sized for the most units that the
+// sequences can make.
+struct Place {
+  int unit, part;                       // unit -1: none
+};
+__device__ __forceinline__ Place place_of(int units, int per) {
+  const int active = units * per;
+  if ((int)blockIdx.x >= active) return Place{-1, 0};
+  const int logical = xcd_contiguous(blockIdx.x, active);
+  return Place{logical / per, logical % per};
+}
+
+// This workgroup's unit, found by every thread; s < 0: there is none.  Up to 64 sequences a wavefront finds it by itself, a sequence a
+// lane.  part: which of the unit's workgroups.
+__device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int per, int& part) {
   __shared__ long long sums[8];
   __shared__ int tmp[8], found[3];
   const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x, n_seqs = a.c.n_seqs;
@@ -59,7 +72,10 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int id, int wan
       const int x = __shfl_up(at, o, kWave), y = __shfl_up(slot, o, kWave);
       if (lane >= o) at += x, slot += y;
     }
-    const unsigned long long ends = __ballot(at > id);
+    const Place p = place_of(__shfl(at, kWave - 1, kWave), per);
+    const int id = p.unit;
+    part = p.part;
+    const unsigned long long ends = id < 0 ? 0 : __ballot(at > id);
     const int s = ends ? __ffsll(ends) - 1 : 0;
     u.s = ends ? s : -1;
     u.units = __shfl(n, s, kWave);
@@ -85,8 +101,19 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int id, int wan
   keys = 0;
   for (int w = 0; w < threads >> 6; ++w) keys += sums[w];
   const long long chunk = chunk_of(keys, want);
-  int before = 0, slots = 0;
+  int n_units = 0;
   for (int b = 0; b < n_seqs; b += threads) {
+    const int s = b + tid;
+    int all;
+    if (s < n_seqs) measure(a, s, u);
+    block_scan(s < n_seqs && u.rows.n > 0 ? units_of(u.total, chunk) : 0, tmp, all);
+    n_units += all;
+  }
+  const Place p = place_of(n_units, per);
+  const int id = p.unit;
+  part = p.part;
+  int before = 0, slots = 0;
+  for (int b = 0; id >= 0 && b < n_seqs; b += threads) {
     const int s = b + tid;
     int n = 0;
     if (s < n_seqs) {
@@ -126,7 +153,7 @@ struct AttnWs {
 };
 
 // Keys and rows of a wide call (more than 64 rows a kv head, bf16, head_dim <= 128), csrc/paged_attn_wide.hip
-constexpr int wide_rows(int halves) { return 256 / halves; }      // rows of a workgroup
-hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, int halves, hipStream_t st);
+constexpr int kWideRows = 128;          // rows of a workgroup
+hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st);
 
 }  // namespace spiffy

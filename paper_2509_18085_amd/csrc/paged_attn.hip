@@ -64,9 +64,9 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
   const int hd = FAST ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
-  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);        // row tiles of the same keys: neighbours on one XCD
-  const int tile = logical % row_tiles, kvh = logical / row_tiles % a.h.Hkv;
-  const Unit u = find_unit(a, logical / row_tiles / a.h.Hkv, want);
+  int place;
+  const Unit u = find_unit(a, want, row_tiles * a.h.Hkv, place);
+  const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * RT * 16;
@@ -495,16 +495,16 @@ int row_tiles_of(const Heads& h, int max_rows) {
   return need < most ? need : most;
 }
 struct Shape {
-  int wide;                 // 0: the kernel of this file, else the halves of csrc/paged_attn_wide.hip
+  bool wide;                // csrc/paged_attn_wide.hip
   int rt, tiles, want, rows;
   long long slots;
 };
 Shape shape_of(const Heads& h, int max_rows) {
   Shape s;
   s.rows = max_rows * (h.Hq / h.Hkv);
-  s.wide = h.f32 || h.hd > 128 || s.rows <= 64 ? 0 : (s.rows <= 128 ? 2 : 1);
+  s.wide = !h.f32 && h.hd <= 128 && s.rows > 64;
   s.rt = row_tiles_of(h, max_rows);
-  s.tiles = cdiv(s.rows, s.wide ? wide_rows(s.wide) : 16 * s.rt);
+  s.tiles = cdiv(s.rows, s.wide ? kWideRows : 16 * s.rt);
   s.want = (s.wide ? kWideGroups : kTargetGroups) / (h.Hkv * s.tiles);
   if (s.want < 1) s.want = 1;
   // a sequence of two units or more has at least 1.5 chunks, so its units are at most 4/3 of its keys over the chunk
@@ -556,7 +556,7 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   ws.o = reinterpret_cast<float*>(p + plan_bytes(a.c) + ml_bytes(a.h, s));
   ws.rows = s.rows;
   hipError_t e;
-  if (s.wide) e = launch_tree_wide(a, ws, s.want, s.tiles, s.wide, st);
+  if (s.wide) e = launch_tree_wide(a, ws, s.want, s.tiles, st);
   else if (a.h.f32) e = a.h.hd <= 64 ? launch_rows<float, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<float, 128>(a, ws, s, st) : launch_rows<float, 256>(a, ws, s, st);
   else e = a.h.hd <= 64 ? launch_rows<bf16_t, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<bf16_t, 128>(a, ws, s, st) : launch_rows<bf16_t, 256>(a, ws, s, st);
   if (e != hipSuccess) return e;

@@ -1,16 +1,19 @@
 // Attention of drafted token trees over a paged cache, many rows a kv head (bf16, head_dim up to 128).
 //
-// With more than 64 rows the matrix instructions are the bound, and a key has to serve them all: eight wavefronts of 32 rows each share
-// tiles of 64 keys through LDS.  HALVES == 1: 256 rows, a wavefront takes all of a tile; HALVES == 2: 128 rows, wavefronts w and w + 4
-// have the same rows and a half of every tile each, joined at the end.
+// With more than 64 rows the matrix instructions are the bound, and a key has to serve them all: eight wavefronts share tiles of 64
+// keys through LDS for 128 rows.  Wavefronts w and w + 4 have the same 32 rows and one half of every tile each; two wavefronts a
+// SIMD, so that one's exponentials run under the other's matrix instructions; they are joined through LDS at the end.
 //
 // S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 instructions.  Accumulator element x of lane (column l32 = lane % 32, half = lane / 32) is
 // key 8 (x / 4) + 4 half + x % 4, so elements 8 i .. 8 i + 7 are the second product's operand of its i-th step as they stand, with V's
 // rows taken in that order by the transposing LDS read (four rows a lane).  Rows lie in LDS as in memory, their 16-byte
 // pieces permuted so that neither kind of read meets a bank twice.
 //
-// Tile t's second product runs against tile t + 1's first: keys are one tile ahead of values in LDS, two tiles ahead of the arithmetic in
-// registers, with one barrier a tile.
+// Step t runs tile t + 1's first product between tile t's exponentials, then tile t's second product.  Keys are one tile ahead of values in
+// LDS and both one more in registers, so a load has a whole step to arrive; one barrier a step.  A row's place in the pool is
+// looked up lane by lane: pages of any size.
+#include <type_traits>
+
 #include "paged_attn.h"
 
 namespace spiffy {
@@ -22,34 +25,38 @@ constexpr int kWideEntries = 4098;                        // pages that are look
 constexpr int kWideKeys = 65536;                          // ... for so many keys at most
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4_ptr_t;
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr_t;
 
-template <int HDP, int HALVES>
+// QUAD: head_dim == HDP, pages of a multiple of the four (64 channels: eight) rows of a wavefront's load lie in one page, their place is the same for all
+// lanes but for a constant.
+template <int HDP, bool QUAD>
 __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnArgs a, const AttnWs ws, int want, int row_tiles, int log_ps) {
-  constexpr int ROWS = wide_rows(HALVES);
-  constexpr int SUB = 2 / HALVES;                         // 32-key tiles of a wavefront
+  constexpr int ROWS = kWideRows;
   constexpr int NK = HDP / 16, NN = HDP / 32;             // steps of the first product, 32-channel tiles of the second
   constexpr int PIECES = HDP / 8, RPT = kTile * PIECES / kThreads;      // 16-byte pieces of a row; rows of a thread
-  constexpr int RSTEP = kThreads / PIECES;
+  constexpr int RSTEP = kThreads / PIECES, WROWS = kWave / PIECES;      // rows of all threads, of a wavefront
   constexpr int ROWB = HDP * 2, TILEB = kTile * ROWB;
   // K tiles 0, 1, V tiles 0, 1; before the new rows the page list, behind it their bits
   __shared__ __align__(16) unsigned char s_kv[4 * TILEB];
   __shared__ __align__(16) int2 s_page[kWideEntries];     // page, rows in it
   __shared__ unsigned long long s_any[SPIFFY_MAX_TREE / 64];
+  __shared__ int s_bad;                                   // the first key of a batch that has no row
   __shared__ unsigned s_odd[kTile / 32];                  // new rows of a tile whose values are not all finite
   const PagedView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
-  const int hd = a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
+  const int hd = QUAD ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
-  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int tile = logical % row_tiles, kvh = logical / row_tiles % a.h.Hkv;
-  const Unit u = find_unit(a, logical / row_tiles / a.h.Hkv, want);
+  int place;
+  const Unit u = find_unit(a, want, row_tiles * a.h.Hkv, place);
+  const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * ROWS;
   if (r0 >= R) return;
   const int lo = (int)(u.index * u.chunk), hi = u.index == u.units - 1 ? u.total : lo + (int)u.chunk;
-  const int group = HALVES == 2 ? wave & 3 : wave, part = HALVES == 2 ? wave >> 2 : 0;
+  const int group = wave & 3, part = wave >> 2;          // which 32 rows, which half of a tile
   const int row = r0 + group * 32 + l32;                  // this lane's column
   const bool busy = r0 + group * 32 < R;                  // the same for the wavefront: it has rows
 
@@ -78,47 +85,39 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   // ---- LDS: where pieces lie, what a lane reads
   auto k_at = [](int r, int piece) { return r * ROWB + 16 * (piece ^ (r & (PIECES - 1))); };
   auto v_at = [](int r, int piece) { return r * ROWB + 16 * (piece ^ ((HDP == 128 ? r & 3 : r >> 1 & 1) << 2)); };
-  auto k_frag = [&](int buf, int sub, int i) {
-    return *reinterpret_cast<const bf16x8*>(s_kv + buf * TILEB + k_at(32 * sub + l32, 2 * i + half));
+  // addresses of a lane's fragments in tile 0; another tile or step is a constant away
+  unsigned ka[NK], va[NN];
+  const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)s_kv;
+#pragma unroll
+  for (int i = 0; i < NK; ++i) ka[i] = lds + k_at(32 * part + l32, 2 * i + half);
+#pragma unroll
+  for (int n = 0; n < NN; ++n) {                          // lane i of 16 names row i / 4, channels 4 (i % 4) ..; it gets channel i of four rows
+    const int r = 32 * part + 4 * half + ((lane & 15) >> 2), ch = 32 * n + 16 * (l32 >> 4) + 4 * (lane & 3);
+    va[n] = lds + 2 * TILEB + v_at(r, ch >> 3) + (ch & 7) * 2;
+  }
+  auto k_frag = [&](int buf, int i) { return *(lds_bf16x8_ptr_t)(size_t)(ka[i] + buf * TILEB); };
+  auto v_half = [&](int buf, int i, int n, int e) {       // keys 16 i + 8 e + 4 half .. + 3 of this half tile, channel 32 n + l32
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(size_t)(va[n] + buf * TILEB + (16 * i + 8 * e) * ROWB));
   };
-  const unsigned v_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)(s_kv + 2 * TILEB);
-  auto v_frag = [&](int buf, int sub, int i, int n) {     // keys 32 sub + 16 i + 8 e + 4 half .. + 3, channel 32 n + l32
-    bf16x8 x;
+  auto joined = [](bf16x4 x, bf16x4 y) { return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7); };
+  auto scores = [&](int buf, f32x16& s) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int r = 32 * sub + 16 * i + 8 * e + 4 * half + ((lane & 15) >> 2), ch = 32 * n + 16 * (l32 >> 4) + 4 * (lane & 3);
-      const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(size_t)(v_base + buf * TILEB + v_at(r, ch >> 3) + (ch & 7) * 2));
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-      for (int z = 0; z < 4; ++z) x[4 * e + z] = y[z];
-    }
-    return x;
-  };
-  auto scores = [&](int buf, f32x16 (&s)[SUB]) {
-#pragma unroll
-    for (int b = 0; b < SUB; ++b) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NK; ++i) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, b + part, i), q[i], s[b], 0, 0, 0);
-    }
+    for (int i = 0; i < NK; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(buf, i), q[i], s, 0, 0, 0);
   };
   // keys that this column does not attend to (a bit a key of the tile)
-  auto hide = [&](f32x16 (&s)[SUB], unsigned long long seen) {
+  auto hide = [&](f32x16& s, unsigned long long seen) {
+    const unsigned bits = (unsigned)(seen >> (32 * part)) >> (4 * half);
 #pragma unroll
-    for (int b = 0; b < SUB; ++b) {
-      const unsigned bits = (unsigned)(seen >> (32 * (b + part))) >> (4 * half);
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (!(bits >> (8 * (e >> 2) + (e & 3)) & 1)) s[b][e] = -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e)
+      if (!(bits >> (8 * (e >> 2) + (e & 3)) & 1)) s[e] = -INFINITY;
   };
-  // as in the kernel for few rows: a column is rescaled when a score passes the maximum in use by 2^8
-  auto soften = [&](f32x16 (&s)[SUB], bf16x8 (&x)[2 * SUB]) {
-    float top = -INFINITY;
+  // as in the kernel for few rows: a column is rescaled when a score passes the maximum in use by 2^8.  Returns the maximum in use.
+  auto follow = [&](const f32x16& s) {
+    float top = s[0];
 #pragma unroll
-    for (int b = 0; b < SUB; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
     top = reduce_32(top, [](float p, float r) { return fmaxf(p, r); }) * scale;
     if (__any(top > m + 8.f)) {
       const float m2 = top > m + 8.f ? top : m, f = weight(m, m2);
@@ -127,23 +126,63 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 #pragma unroll
       for (int n = 0; n < NN; ++n) o[n] *= f;
     }
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int b = 0; b < SUB; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale, -base));
-        l += p;
-        x[2 * b + (e >> 3)][e & 7] = (bf16_t)p;
-      }
+    return m == -INFINITY ? 0.f : m;
   };
-  auto add_values = [&](int buf, const bf16x8 (&x)[2 * SUB]) {
+  // Probabilities 2 i and 2 i + 1, rounded to bf16 (by up to 2^-8 of themselves, as the stored values are), and the sum of what they are then
+  const bf16x2 ones = {(bf16_t)1.f, (bf16_t)1.f};
+  auto soften = [&](const f32x16& s, int i, float base, bf16x8 (&x)[2]) {
+    f32x2 p;
+    p[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i], scale, -base));
+    p[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i + 1], scale, -base));
+    const bf16x2 r = __builtin_convertvector(p, bf16x2);
+    l = __builtin_amdgcn_fdot2_f32_bf16(r, ones, l, false);
+    x[i >> 2][2 * (i & 3)] = r[0];
+    x[i >> 2][2 * (i & 3) + 1] = r[1];
+  };
+  // Second product of one half tile whose scores are s; seen: as for hide
+  auto finish = [&](int buf, f32x16& s, bf16x8 (&x)[2]) {
+    const float base = follow(s);
 #pragma unroll
-    for (int b = 0; b < SUB; ++b)
+    for (int i = 0; i < 8; ++i) soften(s, i, base, x);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int n = 0; n < NN; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(buf, b + part, i, n), x[2 * b + i], o[n], 0, 0, 0);
+      for (int n = 0; n < NN; ++n)
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(v_half(buf, i, n, 0), v_half(buf, i, n, 1)), x[i], o[n], 0, 0, 0);
+  };
+  // Step t of the pipeline, BUF = t % 2: scores `next` of tile t + 1 between the exponentials of s
+  auto step = [&](auto BUF, f32x16& s, f32x16& next) {
+    constexpr int buf = decltype(BUF)::value;
+    bf16x8 k[NK], x[2];
+    bf16x4 v[2][NN][2];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) k[i] = k_frag(1 - buf, i);
+    const float base = follow(s);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) next[e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i < NK) next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i < NK ? i : 0], q[i < NK ? i : 0], next, 0, 0, 0);
+      soften(s, i, base, x);
+      if (i < 2 * NN) {
+        v[i / NN][i % NN][0] = v_half(buf, i / NN, i % NN, 0);
+        v[i / NN][i % NN][1] = v_half(buf, i / NN, i % NN, 1);
+      }
+    }
+    // issue order: a matrix instruction, two exponentials with what is around them, two reads of values
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i < NK) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+      if (i < 2 * NN) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int n = 0; n < NN; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(v[i][n][0], v[i][n][1]), x[i], o[n], 0, 0, 0);
   };
 
   // ---- the cache
@@ -158,6 +197,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     auto entry = [&](int key) { return log_ps >= 0 ? key >> log_ps : (int)((unsigned)key / (unsigned)ps); };
     const int e0 = entry(batch), e1 = entry(end - 1);
     __syncthreads();
+    if (tid == 0) s_bad = end;
+    __syncthreads();
     const int len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += kThreads) {
       const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
@@ -167,61 +208,116 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
         rows = id >= 0 && id < c.n_pages ? clamp_int(len - slot * ps, 0, ps) : 0;
       }
       s_page[e - e0] = make_int2(id, rows);
+      if (rows < ps) atomicMin(&s_bad, e * ps + rows);
     }
     __syncthreads();
-    const int tiles = (end - batch + kTile - 1) / kTile;
+    const int tiles = (end - batch + kTile - 1) / kTile, bad = s_bad;      // below `bad` every key has a row
     // row of the pool that holds a key, -1: none
     auto find = [&](int key) {
       const int e = entry(min(key, end - 1)), off = min(key, end - 1) - e * ps;
       const int2 p = s_page[e - e0];
       return key < end && off < p.y ? p.x * row_of_page + (long long)kvh * ps + off : -1ll;
     };
-    auto load = [&](const bf16_t* pool, int t, u32x4 (&x)[RPT]) {
+    // Where this thread's rows of tile t lie.  QUAD: rows of one wavefront, the first of them; otherwise each lane's piece, -1: none.
+    long long at[RPT];
+    u32x4 kx[RPT], vx[RPT];
+    const int lane_at = (my_row & (WROWS - 1)) * HDP + my_piece * 8;
+    // QUAD: the list's entry is read a step before it is used
+    int2 page[RPT];
+    auto quad_key = [&](int t, int i) {                   // batches begin at multiples of WROWS
+      return min(batch + t * kTile + __builtin_amdgcn_readfirstlane(my_row) + i * RSTEP, end - 1) & -WROWS;
+    };
+    auto look_ahead = [&](int t) {
+      if constexpr (QUAD)
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) page[i] = s_page[entry(quad_key(t, i)) - e0];
+    };
+    auto look_up = [&](int t) {
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
-        const long long r = find(batch + t * kTile + my_row + i * RSTEP);
-        x[i] = r >= 0 && my_piece * 8 < hd ? *reinterpret_cast<const u32x4*>(pool + r * hd + my_piece * 8) : u32x4{};
+        if constexpr (QUAD) {
+          const int key = quad_key(t, i), id = __builtin_amdgcn_readfirstlane(page[i].y > 0 ? page[i].x : 0);
+          at[i] = (id * row_of_page + (long long)kvh * ps + (key - entry(key) * ps)) * HDP;
+        } else {
+          const long long r = find(batch + t * kTile + my_row + i * RSTEP);
+          at[i] = r >= 0 && my_piece * 8 < hd ? r * hd + my_piece * 8 : -1;
+        }
       }
     };
-    auto put_keys = [&](int buf, const u32x4 (&x)[RPT]) {
+    auto load = [&](const bf16_t* pool, u32x4 (&x)[RPT]) {
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + i * RSTEP, my_piece)) = x[i];
+      for (int i = 0; i < RPT; ++i) {
+        if constexpr (QUAD) x[i] = *reinterpret_cast<const u32x4*>(pool + at[i] + lane_at);
+        else x[i] = at[i] >= 0 ? *reinterpret_cast<const u32x4*>(pool + at[i]) : u32x4{};
+      }
     };
-    auto put_values = [&](int buf, const u32x4 (&x)[RPT]) {
+    // rows that are none, or that hold what is none of the sequence's: zeros
+    auto clear = [&](int t, u32x4 (&x)[RPT]) {
+      if (!QUAD || batch + (t + 1) * kTile <= bad) return;
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + (2 + buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = x[i];
+      for (int i = 0; i < RPT; ++i)
+        if (find(batch + t * kTile + my_row + i * RSTEP) < 0) x[i] = u32x4{};
     };
-    u32x4 kx[RPT], vx[RPT];
-    f32x16 s[SUB], next[SUB];
-    load(pk, 0, kx);
-    load(pv, 0, vx);
-    put_keys(0, kx);
-    put_values(0, vx);
+    auto put_keys = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + i * RSTEP, my_piece)) = kx[i];
+    };
+    auto put_values = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + (2 + buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = vx[i];
+    };
+    // tile 0 and the keys of tile 1 into LDS; the keys of tile 2 and the values of tile 1 on their way
+    look_ahead(0);
+    look_up(0);
+    load(pk, kx);
+    load(pv, vx);
+    clear(0, kx);
+    clear(0, vx);
+    put_keys(0);
+    put_values(0);
     if (tiles > 1) {
-      load(pk, 1, kx);
-      put_keys(1, kx);
+      look_ahead(1);
+      look_up(1);
+      load(pk, kx);
+      load(pv, vx);
+      clear(1, kx);
+      put_keys(1);
     }
+    if (tiles > 2) {
+      look_ahead(2);
+      look_up(2);
+      load(pk, kx);
+    }
+    look_ahead(3);
     __syncthreads();
-    if (busy) scores(0, s);
-    for (int t = 0; t < tiles; ++t) {
-      if (t) __syncthreads();                             // keys of tile t + 1 and values of tile t are there, those of t - 1 are done with
-      if (t + 2 < tiles) load(pk, t + 2, kx);
-      if (t + 1 < tiles) load(pv, t + 1, vx);
-      if (busy) {
-        const unsigned long long there = __ballot(find(batch + t * kTile + lane) >= 0);
-        if (there != ~0ull) hide(s, there);
-        bf16x8 x[2 * SUB];
-        if (t + 1 < tiles) scores((t + 1) & 1, next);
-        soften(s, x);
-        add_values(t & 1, x);
-#pragma unroll
-        for (int b = 0; b < SUB; ++b) s[b] = next[b];
-      }
-      if (t + 1 < tiles) put_values((t + 1) & 1, vx);
+    f32x16 sa, sb;
+    if (busy) scores(0, sa);
+    // Step t starts when every wavefront is done with step t - 1: tile t's keys and tile t - 1's values give way to the keys of tile t + 2
+    // and the values of tile t + 1, which the next step's barrier makes visible; those behind them start.
+    auto turn = [&](int t, auto BUF, f32x16& s, f32x16& next) {
+      constexpr int buf = decltype(BUF)::value;
+      __syncthreads();
       if (t + 2 < tiles) {
-        if (t == 0) __syncthreads();                      // tile 0's keys were read in front of the loop
-        put_keys(t & 1, kx);
+        clear(t + 2, kx);
+        put_keys(buf);
       }
+      if (t + 1 < tiles) {
+        clear(t + 1, vx);
+        put_values(1 - buf);
+      }
+      if (t + 2 < tiles) load(pv, vx);
+      if (t + 3 < tiles) {
+        look_up(t + 3);
+        load(pk, kx);
+        look_ahead(t + 4);
+      }
+      if (!busy) return;
+      if (batch + (t + 1) * kTile > bad) hide(s, __ballot(find(batch + t * kTile + lane) >= 0));
+      step(BUF, s, next);                                 // behind the last tile `next` are scores of what LDS holds; nothing reads them
+    };
+    for (int t = 0; t < tiles; t += 2) {
+      turn(t, std::integral_constant<int, 0>{}, sa, sb);
+      if (t + 1 < tiles) turn(t + 1, std::integral_constant<int, 1>{}, sb, sa);
     }
   }
 
@@ -270,35 +366,32 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       __syncthreads();
       const uint64_t seen = bits[(at >> 6) * ROWS + group * 32 + l32];
       if (__any(seen != 0)) {
-        f32x16 s[SUB];
-        bf16x8 x[2 * SUB];
+        f32x16 s;
+        bf16x8 x[2];
         scores(0, s);
         hide(s, seen);
-        soften(s, x);
-        add_values(0, x);
+        finish(0, s, x);
         // values that are not finite, key by key, only in the columns that attend to the key
-        for (int b = 0; b < SUB; ++b) {
-          for (unsigned odd = s_odd[b + part]; odd; odd &= odd - 1) {
-            const int y = __ffs(odd) - 1, key = at + 32 * (b + part) + y;      // owner: half (y / 4) % 2, step y / 16, element 4 (y / 8 % 2) + y % 4
-            const bool mine = seen >> (key & 63) & 1;
-            const bf16_t* from = reinterpret_cast<const bf16_t*>(a.v) + (first + key) * a.kv_stride + kvh * hd;
-            const int slot = 4 * (y >> 3 & 1) + (y & 3);
+        for (unsigned odd = s_odd[part]; odd; odd &= odd - 1) {
+          const int y = __ffs(odd) - 1, key = at + 32 * part + y;      // held by half y / 4 % 2, step y / 16, element 4 (y / 8 % 2) + y % 4
+          const bool mine = seen >> (key & 63) & 1;
+          const bf16_t* from = reinterpret_cast<const bf16_t*>(a.v) + (first + key) * a.kv_stride + kvh * hd;
+          const int slot = 4 * (y >> 3 & 1) + (y & 3);
 #pragma unroll
-            for (int n = 0; n < NN; ++n) {
-              const bf16_t z = 32 * n + l32 < hd && half == (y >> 2 & 1) ? from[32 * n + l32] : (bf16_t)0.f;
-              bf16x8 w, p;
+          for (int n = 0; n < NN; ++n) {
+            const bf16_t z = 32 * n + l32 < hd && half == (y >> 2 & 1) ? from[32 * n + l32] : (bf16_t)0.f;
+            bf16x8 w, p;
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                w[j] = j == slot && !finite_bits(z) ? z : (bf16_t)0.f;
-                p[j] = y >> 4 ? (b ? x[2 * SUB - 1][j] : x[1][j]) : (b ? x[2 * SUB - 2][j] : x[0][j]);
-              }
-              f32x16 more;
-#pragma unroll
-              for (int e = 0; e < 16; ++e) more[e] = 0.f;
-              more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p, more, 0, 0, 0);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[n][e] = mine ? o[n][e] + more[e] : o[n][e];
+            for (int j = 0; j < 8; ++j) {
+              w[j] = j == slot && !finite_bits(z) ? z : (bf16_t)0.f;
+              p[j] = y >> 4 ? x[1][j] : x[0][j];
             }
+            f32x16 more;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) more[e] = 0.f;
+            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p, more, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[n][e] = mine ? o[n][e] + more[e] : o[n][e];
           }
         }
       }
@@ -307,7 +400,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 
   // ---- results: rows of a lane's column, four channels at a time
   float sum = reduce_32(l, [](float p, float r) { return p + r; });
-  if constexpr (HALVES == 2) {
+  {
     // The upper halves' results go through LDS, 32 channels at a time.
     constexpr int LD = 36;
     static_assert(4 * 32 * LD * sizeof(float) <= sizeof(s_kv) && 4 * 32 * sizeof(float2) <= sizeof(s_page), "join buffers");
@@ -353,19 +446,17 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     }
 }
 
-template <int HDP, int HALVES>
-hipError_t launch_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st) {
-  const int ps = a.c.page_size;
-  const long long grid = ((long long)want + a.c.n_seqs) * a.h.Hkv * row_tiles;
-  tree_wide_kernel<HDP, HALVES><<<(unsigned)grid, kThreads, 0, st>>>(a, ws, want, row_tiles, ps & (ps - 1) ? -1 : __builtin_ctz(ps));
-  return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, int halves, hipStream_t st) {
-  if (a.h.hd <= 64) return halves == 2 ? launch_wide<64, 2>(a, ws, want, row_tiles, st) : launch_wide<64, 1>(a, ws, want, row_tiles, st);
-  return halves == 2 ? launch_wide<128, 2>(a, ws, want, row_tiles, st) : launch_wide<128, 1>(a, ws, want, row_tiles, st);
+hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st) {
+  const int ps = a.c.page_size, log_ps = ps & (ps - 1) ? -1 : __builtin_ctz(ps);
+  const unsigned grid = (unsigned)(((long long)want + a.c.n_seqs) * a.h.Hkv * row_tiles);
+  const bool quad = ps % (a.h.hd == 64 ? 8 : 4) == 0;
+  if (a.h.hd == 128 && quad) tree_wide_kernel<128, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
+  else if (a.h.hd == 64 && quad) tree_wide_kernel<64, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
+  else if (a.h.hd > 64) tree_wide_kernel<128, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
+  else tree_wide_kernel<64, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
+  return hipGetLastError();
 }
 
 }  // namespace spiffy
