@@ -4,8 +4,8 @@
 
 namespace spiffy {
 
-constexpr int kAlign = 128;             // keys: unit borders, four wavefronts' steps
-constexpr int kMinChunk = 256;          // keys of a unit at least
+constexpr int kAlign = 128;             // keys of a block: units are whole blocks, four wavefronts' steps
+constexpr int kMinBlocks = 2;           // blocks of a unit at least
 
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ bool finite_bits(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80u) != 0x7f80u; }
@@ -13,29 +13,50 @@ __device__ __forceinline__ bool finite_bits(bf16_t x) { return (__builtin_bit_ca
 // Weight of a partial result whose maximum is m in one whose maximum is top (logarithms to base 2)
 __device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : __builtin_amdgcn_exp2f(m - top); }
 
-struct Unit {
-  int s, index, units, slot;            // slot of the sequence's first partial result
-  long long chunk;
+// A sequence's keys are numbered through its cache, then, from a block's border on, through its new rows.  `blocks` is what they
+// cost: a last block of new rows that is not full counts nothing (one token must not make a block of its own) and goes with the last unit.
+struct Keys {
   RowRange rows;
   int eff, tree0, total;                // keys of the cache, number of the first new row, end of the numbering
+  int blocks;
+};
+// One unit: blocks first .. of them are divided evenly
+struct Unit : Keys {
+  int s, index, units, slot;            // slot of the sequence's first partial result
+  __device__ __forceinline__ int border(int i) const { return (int)((long long)i * blocks / units) * kAlign; }
+  __device__ __forceinline__ int lo() const { return border(index); }
+  __device__ __forceinline__ int hi() const { return index == units - 1 ? total : border(index + 1); }
 };
 
-__device__ __forceinline__ void measure(const TreeAttnArgs& a, int s, Unit& u) {
-  u.rows = rows_of(a.rows, s);
-  if (u.rows.n > a.max_rows) u.rows.n = a.max_rows;
+__device__ __forceinline__ Keys keys_of(const TreeAttnArgs& a, int s) {
+  Keys k;
+  k.rows = rows_of(a.rows, s);
+  if (k.rows.n > a.max_rows) k.rows.n = a.max_rows;
   // below 2^31 - 2^16 (checked on the host), so that numbers of new rows and of batches fit behind it
-  u.eff = a.selected ? a.n_sel * a.c.page_size : seq_len(a.c, s);
-  u.tree0 = (u.eff + kAlign - 1) / kAlign * kAlign;
-  u.total = u.tree0 + u.rows.n;
+  k.eff = a.selected ? a.n_sel * a.c.page_size : seq_len(a.c, s);
+  const int cache = (k.eff + kAlign - 1) / kAlign, blocks = cache + k.rows.n / kAlign;
+  k.tree0 = cache * kAlign;
+  k.total = k.tree0 + k.rows.n;
+  k.blocks = k.rows.n > 0 ? (blocks > 0 ? blocks : 1) : 0;
+  return k;
 }
-__device__ __forceinline__ int units_of(int total, long long chunk) {
-  const int n = (int)((total + chunk / 2) / chunk);
-  return n < 1 ? 1 : n;
+// Units of at most `most` blocks
+__device__ __forceinline__ int units_of(int blocks, int most) { return (int)(((unsigned)blocks + most - 1) / most); }
+__device__ __forceinline__ int most_of(long long blocks, int want) {
+  const long long most = (blocks + want - 1) / want;      // 4096 sequences of 2^24 blocks: 36 bits, an int's only with `want` of 32 and more
+  return most < kMinBlocks ? kMinBlocks : (most > (1 << 25) ? 1 << 25 : (int)most);
 }
 
-__device__ __forceinline__ long long chunk_of(long long keys, int want) {
-  const long long chunk = ((keys + want - 1) / want + kAlign - 1) / kAlign * kAlign;
-  return chunk < kMinChunk ? kMinChunk : chunk;
+// Sum over the lanes up to and with this one, on vector instructions (rows of 16 lanes, then the last lane of one or two rows to the next)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xF>(x);      // row_shr:1, 2, 4, 8
+  x = dpp_add<0x112, 0xF>(x);
+  x = dpp_add<0x114, 0xF>(x);
+  x = dpp_add<0x118, 0xF>(x);
+  x = dpp_add<0x142, 0xA>(x);      // row_bcast:15 to rows 1 and 3
+  return dpp_add<0x143, 0xC>(x);   // row_bcast:31 to rows 2 and 3
 }
 
 // A workgroup's part of a call: `per` workgroups (kv heads times row tiles) a unit, those of one unit next to each other on one XCD.  Only
@@ -52,87 +73,76 @@ __device__ __forceinline__ Place place_of(int units, int per) {
 }
 
 // This workgroup's unit, found by every thread; s < 0: there is none.  Up to 64 sequences a wavefront finds it by itself, a sequence a
-// lane.  part: which of the unit's workgroups.
+// lane.  There can be up to one unit a sequence more than `want`.  ONE_ROUND: `want` fills the GPU once, so the units of up to `want`
+// sequences grow until there are no more (16 trees over 3000 to 4100 rows, 32 units wanted: 81 us with the 48 that there were, 55
+// with 32).  part: which of the unit's workgroups.
+template <bool ONE_ROUND>
 __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int per, int& part) {
   __shared__ long long sums[8];
   __shared__ int tmp[8], found[3];
   const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x, n_seqs = a.c.n_seqs;
   Unit u;
   if (n_seqs <= kWave) {
-    u.rows.n = u.total = 0;
-    if (lane < n_seqs) measure(a, lane, u);
-    long long keys = u.rows.n > 0 ? u.total : 0;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) keys += __shfl_xor(keys, o, kWave);
-    u.chunk = chunk_of(keys, want);
-    const int n = u.rows.n > 0 ? units_of(u.total, u.chunk) : 0;
-    int at = n, slot = n > 1 ? n : 0;                      // sums up to and with this sequence
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int x = __shfl_up(at, o, kWave), y = __shfl_up(slot, o, kWave);
-      if (lane >= o) at += x, slot += y;
+    Keys k = keys_of(a, lane < n_seqs ? lane : 0);
+    const int blocks = lane < n_seqs ? k.blocks : 0;      // 64 times 2^24 of them fit
+    int most = most_of(__builtin_amdgcn_readlane(wave_scan(blocks), kWave - 1), want);
+    int n = units_of(blocks, most), at = wave_scan(n);
+    for (int i = 0; ONE_ROUND && i < 8 && n_seqs <= want && __builtin_amdgcn_readlane(at, kWave - 1) > want; ++i) {
+      most += most / 8 + 1;
+      n = units_of(blocks, most);
+      at = wave_scan(n);
     }
-    const Place p = place_of(__shfl(at, kWave - 1, kWave), per);
-    const int id = p.unit;
+    const int slot = wave_scan(n > 1 ? n : 0);            // like `at`: up to and with this sequence
+    const Place p = place_of(__builtin_amdgcn_readlane(at, kWave - 1), per);
     part = p.part;
-    const unsigned long long ends = id < 0 ? 0 : __ballot(at > id);
+    const unsigned long long ends = p.unit < 0 ? 0 : __ballot(at > p.unit);
     const int s = ends ? __ffsll(ends) - 1 : 0;
     u.s = ends ? s : -1;
-    u.units = __shfl(n, s, kWave);
-    u.index = id - (__shfl(at, s, kWave) - u.units);
-    u.slot = __shfl(slot, s, kWave) - (u.units > 1 ? u.units : 0);
-    u.rows.first = __shfl(u.rows.first, s, kWave);
-    u.rows.n = __shfl(u.rows.n, s, kWave);
-    u.eff = __shfl(u.eff, s, kWave);
-    u.tree0 = __shfl(u.tree0, s, kWave);
-    u.total = __shfl(u.total, s, kWave);
+    u.units = __builtin_amdgcn_readlane(n, s);
+    u.index = p.unit - (__builtin_amdgcn_readlane(at, s) - u.units);
+    u.slot = __builtin_amdgcn_readlane(slot, s) - (u.units > 1 ? u.units : 0);
+    u.rows.first = __builtin_amdgcn_readlane(k.rows.first, s);
+    u.rows.n = __builtin_amdgcn_readlane(k.rows.n, s);
+    u.eff = __builtin_amdgcn_readlane(k.eff, s);
+    u.tree0 = __builtin_amdgcn_readlane(k.tree0, s);
+    u.total = __builtin_amdgcn_readlane(k.total, s);
+    u.blocks = __builtin_amdgcn_readlane(k.blocks, s);
     return u;
   }
-  long long keys = 0;
-  for (int s = tid; s < n_seqs; s += threads) {
-    measure(a, s, u);
-    if (u.rows.n > 0) keys += u.total;
-  }
+  long long blocks = 0;
+  for (int s = tid; s < n_seqs; s += threads) blocks += keys_of(a, s).blocks;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) keys += __shfl_xor(keys, o, kWave);
-  if (lane == 0) sums[tid >> 6] = keys;
+  for (int o = 32; o; o >>= 1) blocks += __shfl_xor(blocks, o, kWave);
+  if (lane == 0) sums[tid >> 6] = blocks;
   if (tid == 0) found[0] = -1;
   __syncthreads();
-  keys = 0;
-  for (int w = 0; w < threads >> 6; ++w) keys += sums[w];
-  const long long chunk = chunk_of(keys, want);
+  blocks = 0;
+  for (int w = 0; w < threads >> 6; ++w) blocks += sums[w];
+  const int most = most_of(blocks, want);
   int n_units = 0;
   for (int b = 0; b < n_seqs; b += threads) {
     const int s = b + tid;
     int all;
-    if (s < n_seqs) measure(a, s, u);
-    block_scan(s < n_seqs && u.rows.n > 0 ? units_of(u.total, chunk) : 0, tmp, all);
+    block_scan(s < n_seqs ? units_of(keys_of(a, s).blocks, most) : 0, tmp, all);
     n_units += all;
   }
   const Place p = place_of(n_units, per);
-  const int id = p.unit;
   part = p.part;
   int before = 0, slots = 0;
-  for (int b = 0; id >= 0 && b < n_seqs; b += threads) {
-    const int s = b + tid;
-    int n = 0;
-    if (s < n_seqs) {
-      measure(a, s, u);
-      n = u.rows.n > 0 ? units_of(u.total, chunk) : 0;
-    }
+  for (int b = 0; p.unit >= 0 && b < n_seqs; b += threads) {
+    const int s = b + tid, n = s < n_seqs ? units_of(keys_of(a, s).blocks, most) : 0;
     int all, all_slots;
     const int at = before + block_scan(n, tmp, all), slot = slots + block_scan(n > 1 ? n : 0, tmp, all_slots);
-    if (id >= at && id < at + n) found[0] = s, found[1] = at, found[2] = slot;
+    if (p.unit >= at && p.unit < at + n) found[0] = s, found[1] = at, found[2] = slot;
     before += all;
     slots += all_slots;
   }
   __syncthreads();
   u.s = found[0];
   if (u.s < 0) return u;
-  measure(a, u.s, u);
-  u.chunk = chunk;
-  u.units = units_of(u.total, chunk);
-  u.index = id - found[1];
+  static_cast<Keys&>(u) = keys_of(a, u.s);
+  u.units = units_of(u.blocks, most);
+  u.index = p.unit - found[1];
   u.slot = found[2];
   return u;
 }

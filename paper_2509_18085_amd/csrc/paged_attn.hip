@@ -10,18 +10,20 @@
 // workgroup use the same ones.
 //
 // Work is cut along the keys.  A sequence's keys are numbered through its cache (pages in table order, or the selected pages), then, from
-// a multiple of 128 on, its new rows; every sequence is cut into units of about `chunk` keys, chunk being the whole call's keys over
-// the number of units that fill the GPU, so a long sequence beside short ones is spread over all of it.  The four wavefronts
-// of a unit take steps of 32 (fp32: 16) keys in turn, each with its own running maximum and sum; they are joined in LDS, and units of one
-// sequence by a second kernel, always in the same order.
+// a multiple of 128 on, its new rows, and divided evenly into as many units as its share of the call's keys, so a long sequence
+// beside short ones is spread over all of the GPU.  The four wavefronts of a unit take steps of 32 (fp32: 16) keys in turn, each with
+// its own running maximum and sum; they are joined in LDS, and units of one sequence by a second kernel, always in the same order.
 #include "paged_attn.h"
 
 namespace spiffy {
 
 namespace {
 
-constexpr int kTargetGroups = 1024;     // workgroups that the units of a call are to make
-constexpr int kWideGroups = 256;        // ... of the wide kernel, one a CU
+// Workgroups that the units of a call are to make.  Four row tiles take a CU for one workgroup, two leave no room for a third, and more than one round of them only adds
+// starts and joins (one tree of 16 tokens over 131001 rows, 256 / 512 / 1024: 105 / 116 / 142 us; 16 trees over 3000 to 4100 rows 55 / 65 /
+// 83); one row tile leaves room for two or three and wants a second round where lengths differ.
+constexpr int target_groups(int rt) { return rt > 1 ? 256 : 1024; }
+constexpr int kWideGroups = 256;        // the wide kernel: one workgroup a CU
 constexpr int kEntries = 1026;          // pages that are looked up at a time
 constexpr int kBatch = 1024;            // ... by keys: pages of one row, and
 constexpr int kBatchFast = 16384;       // pages of 16 rows, from an entry's middle to another's
@@ -65,13 +67,13 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   const int hd = FAST ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
   int place;
-  const Unit u = find_unit(a, want, row_tiles * a.h.Hkv, place);
+  const Unit u = find_unit<(RT > 1)>(a, want, row_tiles * a.h.Hkv, place);
   const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * RT * 16;
   if (r0 >= R) return;
-  const int lo = (int)(u.index * u.chunk), hi = u.index == u.units - 1 ? u.total : lo + (int)u.chunk;
+  const int lo = u.lo(), hi = u.hi();
 
   // The scale is taken as positive; its sign goes to the queries, and a scale of zero makes them zero.
   const float sign = a.scale > 0.f ? 1.f : (a.scale < 0.f ? -1.f : 0.f);
@@ -505,10 +507,11 @@ Shape shape_of(const Heads& h, int max_rows) {
   s.wide = !h.f32 && h.hd <= 128 && s.rows > 64;
   s.rt = row_tiles_of(h, max_rows);
   s.tiles = cdiv(s.rows, s.wide ? kWideRows : 16 * s.rt);
-  s.want = (s.wide ? kWideGroups : kTargetGroups) / (h.Hkv * s.tiles);
+  s.want = (s.wide ? kWideGroups : target_groups(s.rt)) / (h.Hkv * s.tiles);
   if (s.want < 1) s.want = 1;
-  // a sequence of two units or more has at least 1.5 chunks, so its units are at most 4/3 of its keys over the chunk
-  s.slots = 4ll * s.want / 3 + 2;
+  // a sequence of two units or more has more than one full one, so its units are less than twice its blocks over a unit's, and all
+  // blocks over a unit's are `want` at most
+  s.slots = 2ll * s.want + 2;
   return s;
 }
 size_t plan_bytes(const PagedView& c) { return align_up(sizeof(int2) * (size_t)c.n_seqs, 256); }
@@ -561,8 +564,8 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   else e = a.h.hd <= 64 ? launch_rows<bf16_t, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<bf16_t, 128>(a, ws, s, st) : launch_rows<bf16_t, 256>(a, ws, s, st);
   if (e != hipSuccess) return e;
   // no sequence can have more than one unit: nothing to join
-  const long long most = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size + kAlign + a.max_rows;
-  if (2 * most < 3 * kMinChunk) return hipSuccess;
+  const long long cache = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size;
+  if ((cache + kAlign - 1) / kAlign + a.max_rows / kAlign <= kMinBlocks) return hipSuccess;
   // few rows have many partial results each and wait for them: four wavefronts a row; many rows: one
   const dim3 grid(a.rows.T, a.h.Hq);
   const int threads = (long long)a.rows.T * a.h.Hq <= 2048 ? 256 : 64;

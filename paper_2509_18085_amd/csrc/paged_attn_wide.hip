@@ -49,13 +49,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   const int hd = QUAD ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
   int place;
-  const Unit u = find_unit(a, want, row_tiles * a.h.Hkv, place);
+  const Unit u = find_unit<true>(a, want, row_tiles * a.h.Hkv, place);
   const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * ROWS;
   if (r0 >= R) return;
-  const int lo = (int)(u.index * u.chunk), hi = u.index == u.units - 1 ? u.total : lo + (int)u.chunk;
+  const int lo = u.lo(), hi = u.hi();
   const int group = wave & 3, part = wave >> 2;          // which 32 rows, which half of a tile
   const int row = r0 + group * 32 + l32;                  // this lane's column
   const bool busy = r0 + group * 32 < R;                  // the same for the wavefront: it has rows

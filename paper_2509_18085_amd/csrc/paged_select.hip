@@ -12,8 +12,6 @@ template <typename T> struct Piece;       // 16 bytes of a row
 template <> struct Piece<float> { typedef f32x4 type; static constexpr int n = 4; };
 template <> struct Piece<bf16_t> { typedef bf16x8 type; static constexpr int n = 8; };
 
-constexpr int kSeqChunk = SPIFFY_MAX_SEQS / 256;
-
 // A wavefront a (page, kv head, layer): 64 / (16-byte pieces of a row) rows at a time, the row groups joined at the end.
 template <typename T>
 __global__ __launch_bounds__(256) void page_summary_kernel(const SummaryArgs a) {
@@ -86,39 +84,95 @@ __global__ __launch_bounds__(256) void page_summary_kernel(const SummaryArgs a) 
   }
 }
 
-// Scores of 64 pages (a lane each) of one (sequence, kv head); the four wavefronts share the rows.  Sums are fp64.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ bool finite_value(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Scores of 16 pages of one (sequence, kv head) a wavefront, on fp64 matrix instructions: with q+ = max(q, 0) and q- = min(q, 0) a bound is
+// q+ . hi + q- . lo.  Operand A is 16 rows by 4 channels, B 4 channels by 16 pages; group grp of 16 lanes takes the 16-byte pieces
+// 4 i + grp of a row, element e of all four at once, so no operand needs another lane's data.  Which accumulator is which row
+// does not matter: only the maximum over the rows is wanted, and rows beyond the last repeat it.  Up to kRowTiles row
+// tiles go over a page's summary at once.  0 * inf is not what the bound means: 16 pages with a summary that is not finite are
+// scored element by element instead.
+constexpr int kRowTiles = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void page_score_kernel(const SelectArgs a) {
-  __shared__ double best[4][kWave];
+  typedef typename Piece<T>::type piece_t;
+  constexpr int N = Piece<T>::n;
   const PagedView& c = a.c;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = a.h.Hq / a.h.Hkv, hd = a.h.hd;
-  const int kvh = blockIdx.y, s = blockIdx.z, slot = blockIdx.x * kWave + lane;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, grp = lane >> 4, g = a.h.Hq / a.h.Hkv, hd = a.h.hd;
+  const int kvh = blockIdx.y, s = blockIdx.z, slot = (blockIdx.x * 4 + wave) * 16 + l16;
   const int used = pages_of(seq_len(c, s), c.page_size);
-  if ((int)blockIdx.x * kWave >= used) return;
+  if (slot - l16 >= used) return;
   const RowRange r = rows_of(a.rows, s);
-  const int n = (r.n < a.max_rows ? r.n : a.max_rows) * g;
+  const int R = (r.n < a.max_rows ? r.n : a.max_rows) * g;
   const int page = slot < used ? c.table[(long long)s * c.max_pages + slot] : -1;
   const bool there = page >= 0 && page < c.n_pages;
-  const T* sum = reinterpret_cast<const T*>(a.summary) + ((long long)(there ? page : 0) * a.h.Hkv + kvh) * 2 * hd;
+  const T* lo = reinterpret_cast<const T*>(a.summary) + ((long long)(there ? page : 0) * a.h.Hkv + kvh) * 2 * hd;
+  auto row = [&](int i) {
+    return reinterpret_cast<const T*>(a.q) + (long long)(r.first + i / g) * a.q_stride + (kvh * g + i % g) * hd;
+  };
   double top = -INFINITY;
-  for (int i = wave; i < n; i += 4) {
-    const T* q = reinterpret_cast<const T*>(a.q) + (r.first + i / g) * a.q_stride + (kvh * g + i % g) * hd;
-    double x = 0;
-    for (int ch = 0; ch < hd; ++ch) {
-      const float v = to_f32(q[ch]);
-      x += (double)v * (double)to_f32(sum[(v > 0.f ? hd : 0) + ch]);
-    }
-    top = x > top ? x : top;
-  }
-  best[wave][lane] = top;
-  __syncthreads();
-  if (wave == 0 && slot < used) {
+  bool odd = false;
+  for (int r0 = 0; r0 < R && !odd; r0 += 16 * kRowTiles) {
+    const int tiles = min(kRowTiles, (R - r0 + 15) / 16);
+    f64x4 x[kRowTiles];
+    const T* q[kRowTiles];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) top = best[w][lane] > top ? best[w][lane] : top;
-    if (!there) top = -INFINITY;
-    if (slot < a.keep_first || slot >= used - a.keep_last) top = INFINITY;
-    a.scores[((long long)s * a.h.Hkv + kvh) * c.max_pages + slot] = top;
+    for (int t = 0; t < kRowTiles; ++t) {
+      x[t] = f64x4{0., 0., 0., 0.};
+      q[t] = row(min(r0 + 16 * t + l16, R - 1));
+    }
+    for (int i = 0; 4 * N * i < hd; ++i) {
+      const int ch = (4 * i + grp) * N;
+      const bool in = ch < hd;
+      const piece_t least = in ? *reinterpret_cast<const piece_t*>(lo + ch) : piece_t{};
+      const piece_t most = in ? *reinterpret_cast<const piece_t*>(lo + hd + ch) : piece_t{};
+      piece_t row_piece[kRowTiles];
+#pragma unroll
+      for (int t = 0; t < kRowTiles; ++t) row_piece[t] = in && t < tiles ? *reinterpret_cast<const piece_t*>(q[t] + ch) : piece_t{};
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float l = to_f32((T)least[e]), m = to_f32((T)most[e]);
+        odd |= there && !(finite_value(l) && finite_value(m));
+        const double dl = (double)l, dm = (double)m;
+#pragma unroll
+        for (int t = 0; t < kRowTiles; ++t) {
+          if (t >= tiles) break;
+          const float v = to_f32((T)row_piece[t][e]);
+          const bool up = v > 0.f;                         // NaN goes with the negative ones and makes the row's score NaN
+          x[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(up ? v : 0.f), dm, x[t], 0, 0, 0);
+          x[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(up ? 0.f : v), dl, x[t], 0, 0, 0);
+        }
+      }
+    }
+    odd = __any(odd);
+#pragma unroll
+    for (int t = 0; t < kRowTiles; ++t)
+      if (t < tiles)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = x[t][e] > top ? x[t][e] : top;
   }
+  if (odd) {                                               // the four groups share the rows
+    top = -INFINITY;
+    for (int i = grp; i < R; i += 4) {
+      const T* q = row(i);
+      double x = 0;
+      for (int ch = 0; ch < hd; ++ch) {
+        const float v = to_f32(q[ch]);
+        x += (double)v * (double)to_f32(lo[(v > 0.f ? hd : 0) + ch]);
+      }
+      top = x > top ? x : top;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o < kWave; o <<= 1) {
+    const double y = __shfl_xor(top, o, kWave);
+    top = y > top ? y : top;
+  }
+  if (!there) top = -INFINITY;
+  if (slot < a.keep_first || slot >= used - a.keep_last) top = INFINITY;
+  if (grp == 0 && slot < used) a.scores[((long long)s * a.h.Hkv + kvh) * c.max_pages + slot] = top;
 }
 
 // Order of doubles as order of unsigned integers
@@ -127,12 +181,15 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
   return b >> 63 ? ~b : b | 1ull << 63;
 }
 
-// One workgroup a (sequence, kv head): the n_sel-th highest score digit by digit (8 bits a pass), then the pages above it and the first
-// ones equal to it in ascending order.
-constexpr int kPickThreads = 512;
+// One workgroup a (sequence, kv head): the n_sel-th highest score is found digit by digit, 12 bits a pass, until a digit's pages are all
+// taken; the first digit is sign and exponent, the second already tells a few hundred pages apart, so it takes two or three
+// passes (8-bit digits took four to five, all eight of them without the early end 12 us at 521 pages, counting every page against all others in LDS 25).  Then the
+// pages above and the first ones equal to it are written in ascending order.  Up to kKeep pages a thread the scores stay in registers.
+constexpr int kPickThreads = 512, kDigit = 12, kBins = 1 << kDigit, kKeep = 8;
 __global__ __launch_bounds__(kPickThreads) void page_pick_kernel(const SelectArgs a) {
-  __shared__ int hist[256], tmp[kPickThreads / 64];
-  __shared__ int s_digit, s_left;
+  __shared__ __align__(16) int hist[kBins];
+  __shared__ int tmp[kPickThreads / 64];
+  __shared__ int s_digit, s_left, s_here;
   const PagedView& c = a.c;
   const int tid = threadIdx.x, kvh = blockIdx.x, s = blockIdx.y;
   const int used = pages_of(seq_len(c, s), c.page_size);
@@ -140,41 +197,62 @@ __global__ __launch_bounds__(kPickThreads) void page_pick_kernel(const SelectArg
   const double* score = a.scores + list * c.max_pages;
   int32_t* out = a.selected + list * a.n_sel;
   const int n = a.n_sel < used ? a.n_sel : used;
+  for (int j = n + tid; j < a.n_sel; j += kPickThreads) out[j] = -1;
+  if (n == used) {
+    for (int j = tid; j < used; j += kPickThreads) out[j] = j;
+    return;
+  }
+  unsigned long long kept[kKeep];
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i) kept[i] = tid + i * kPickThreads < used ? order_of(score[tid + i * kPickThreads]) : 0;
+  const int rounds = (used + kPickThreads - 1) / kPickThreads;
   unsigned long long prefix = 0, known = 0;        // the digits found so far, and which bits they are
   int left = n;                                    // pages still to find among those with these digits
-  if (n < used) {
-    for (int shift = 56; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int j = tid; j < used; j += kPickThreads) {
-        const unsigned long long o = order_of(score[j]);
-        if ((o & known) == prefix) atomicAdd(&hist[o >> shift & 255], 1);
-      }
-      __syncthreads();
-      int total;
-      const int mine = tid < 256 ? hist[255 - tid] : 0;             // the highest digit first
-      const int before = block_scan(mine, tmp, total);
-      if (tid < 256 && before < left && left <= before + mine) s_digit = 255 - tid, s_left = left - before;
-      __syncthreads();
-      prefix |= (unsigned long long)s_digit << shift;
-      known |= 255ull << shift;
-      left = s_left;
+  for (int shift = 64 - kDigit; ; shift = shift > kDigit ? shift - kDigit : 0) {
+    const unsigned long long digit = (kBins - 1ull) & ~(known >> shift);      // the last one is shorter
+#pragma unroll
+    for (int i = 0; i < kBins / kPickThreads; ++i) hist[tid + i * kPickThreads] = 0;
+    __syncthreads();
+    auto count = [&](int j, unsigned long long o) {
+      if (j < used && (o & known) == prefix) atomicAdd(&hist[o >> shift & digit], 1);
+    };
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i)
+      if (i < rounds) count(tid + i * kPickThreads, kept[i]);
+    for (int i = kKeep; i < rounds; ++i) {
+      const int j = tid + i * kPickThreads;
+      count(j, j < used ? order_of(score[j]) : 0);
     }
+    __syncthreads();
+    int bins[kBins / kPickThreads], mine = 0, total;               // this thread's bins, the highest first
+#pragma unroll
+    for (int i = 0; i < kBins / kPickThreads; ++i) mine += bins[i] = hist[kBins - 1 - (tid * (kBins / kPickThreads) + i)];
+    int before = block_scan(mine, tmp, total);
+#pragma unroll
+    for (int i = 0; i < kBins / kPickThreads; ++i) {
+      if (before < left && left <= before + bins[i])
+        s_digit = kBins - 1 - (tid * (kBins / kPickThreads) + i), s_left = left - before, s_here = bins[i];
+      before += bins[i];
+    }
+    __syncthreads();
+    prefix |= (unsigned long long)s_digit << shift;
+    known |= digit << shift;
+    left = s_left;
+    if (left == s_here || shift == 0) break;       // all that have these digits, or as many of equal ones
   }
   int done = 0, ties = 0;
-  for (int b = 0; b < used && n; b += kPickThreads) {
-    const int j = b + tid;
-    const unsigned long long o = j < used ? order_of(score[j]) : 0;
-    const bool more = j < used && (n == used || o > prefix), tie = j < used && n < used && o == prefix;
+  for (int i = 0; i < rounds; ++i) {
+    const int j = i * kPickThreads + tid;
+    unsigned long long o = j < used ? order_of(score[j]) & known : 0;
+    const bool tie = j < used && o == prefix;
     int t_all, all;
     const int t = ties + block_scan(tie, tmp, t_all);
-    const bool take = more || (tie && t < left);
+    const bool take = j < used && (o > prefix || (tie && t < left));
     const int at = done + block_scan(take, tmp, all);
     if (take && at < n) out[at] = j;
     ties += t_all;
     done += all;
   }
-  for (int j = n + tid; j < a.n_sel; j += kPickThreads) out[j] = -1;
 }
 
 }  // namespace
@@ -190,7 +268,7 @@ size_t page_select_workspace_bytes(const PagedView& c, const Heads& h) {
   return sizeof(double) * (size_t)c.n_seqs * h.Hkv * c.max_pages;
 }
 hipError_t launch_page_select(const SelectArgs& a, hipStream_t st) {
-  const dim3 grid(cdiv(a.c.max_pages, kWave), a.h.Hkv, a.c.n_seqs);
+  const dim3 grid(cdiv(a.c.max_pages, kWave), a.h.Hkv, a.c.n_seqs);      // 16 pages a wavefront
   if (a.h.f32) page_score_kernel<float><<<grid, 256, 0, st>>>(a);
   else page_score_kernel<bf16_t><<<grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();

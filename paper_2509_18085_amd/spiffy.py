@@ -602,6 +602,10 @@ def tree_mask(edges, n: int, device="cuda") -> torch.Tensor:
     return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in words], dtype=torch.int64, device=device)
 
 
+# the current stream's handle without the Python object around it (some 3 us a call), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 class PagedCache:
     """A cache of pages that sequences share, and the attention of drafted token trees over it (spiffy_pages_*, spiffy_page_*,
     spiffy_tree_attention).
@@ -620,7 +624,7 @@ class PagedCache:
             raise ValueError("refs is [n_pages], table [n_seqs, max_pages], len [n_seqs]")
         if summary is not None and tuple(summary.shape) != (*k.shape[:3], 2, k.shape[4]):
             raise ValueError("summary is [n_layers, n_pages, Hkv, 2, hd]")
-        self.device, self._dt = k.device, _tdtype(cfg)
+        self.device, self._dt, self._index = k.device, _tdtype(cfg), k.device.index
         for t in (k, v) if summary is None else (k, v, summary):
             self._typed(t, self._dt)
         for t in (refs, table, len):
@@ -633,6 +637,7 @@ class PagedCache:
         self._layers = (PageLayer * max(1, self.n_layers))(*[PageLayer(_ptr(k) + l * step, _ptr(v) + l * step, None if summary is None else _ptr(summary) + l * sstep)
                                                              for l in range(self.n_layers)])
         self._cfg, self._cache = C.byref(self.cfg), C.byref(self._struct)
+        self._layer_refs = [C.byref(x) for x in self._layers]
         self._pages_ws = int(lib.spiffy_pages_workspace_bytes(self._cache))
         self._select_ws = int(lib.spiffy_page_select_workspace_bytes(self._cfg, self._cache))
         if not self._pages_ws or not self._select_ws:
@@ -655,25 +660,23 @@ class PagedCache:
             raise ValueError("expected %s on %s, got %s on %s" % (dtype, self.device, t.dtype, t.device))
         return _ptr(t)
 
-    def _ints(self, t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
+    def _ints(self, t: Optional[torch.Tensor], n: int) -> Optional[int]:
         if t is None:
             return None
-        if t.dim() != 1 or (n is not None and t.shape[0] != n):
-            raise ValueError("expected [%s] int32, got %s" % ("n" if n is None else n, tuple(t.shape)))
+        if t.dim() != 1 or t.shape[0] != n:
+            raise ValueError("expected [%d] int32, got %s" % (n, tuple(t.shape)))
         return self._typed(t, torch.int32)
 
-    def _rows(self, t: torch.Tensor, heads: int, T: Optional[int] = None) -> int:
-        """[T, heads, hd] with rows of any stride; the heads of a row lie side by side."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.cfg.head_dim or (T is not None and t.shape[0] != T):
-            raise ValueError("expected [%s, %d, %d], got %s" % ("T" if T is None else T, heads, self.cfg.head_dim, tuple(t.shape)))
+    def _rows(self, t: torch.Tensor, heads: int, T: int) -> int:
+        """Stride of the rows of [T, heads, hd]; the heads of a row lie side by side."""
+        hd, shape, stride = self.cfg.head_dim, t.shape, t.stride()
+        if len(shape) != 3 or shape[0] != T or shape[1] != heads or shape[2] != hd:
+            raise ValueError("expected [%d, %d, %d], got %s" % (T, heads, hd, tuple(shape)))
         if t.dtype != self._dt or t.device != self.device:
             raise ValueError("expected %s on %s, got %s on %s" % (self._dt, self.device, t.dtype, t.device))
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.cfg.head_dim):
+        if T > 0 and (stride[2] != 1 or (heads > 1 and stride[1] != hd)):
             raise ValueError("the heads of a row lie side by side")
-        return self._stride(t, 0, heads)
-
-    def _stride(self, t: torch.Tensor, dim: int, heads: int) -> int:
-        return t.stride(dim) if t.shape[dim] > 1 else heads * self.cfg.head_dim      # of one row torch may say anything
+        return stride[0] if T > 1 else heads * hd             # of one row torch may say anything
 
     def _mask(self, mask: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
         if mask is None:
@@ -685,17 +688,26 @@ class PagedCache:
     def _layer(self, layer: int):
         if not 0 <= layer < self.n_layers:
             raise IndexError("layer %d of %d" % (layer, self.n_layers))
-        return C.byref(self._layers[layer])
+        return self._layer_refs[layer]
 
-    def _call(self, workspace_bytes: int, workspace: Optional[torch.Tensor], stream, call):
-        """call(workspace pointer, its bytes, stream) on the cache's device, in the stream's allocator."""
+    def _elsewhere(self, stream) -> bool:
+        return stream is not None or torch.cuda.current_device() != self._index
+
+    def _current(self) -> Optional[int]:
+        return (_raw_stream(self._index) if _raw_stream else torch.cuda.current_stream().cuda_stream) or None
+
+    def _there(self, stream, call, *args, **kw):
+        """The call on the cache's device and on that stream (a torch stream or a raw handle), whose allocator it then uses."""
         with torch.cuda.device(self.device):
             if stream is not None and not hasattr(stream, "cuda_stream"):
                 stream = torch.cuda.ExternalStream(int(stream), device=self.device) if int(stream) else torch.cuda.default_stream(self.device)
-            with torch.cuda.stream(stream):                       # None: the current one
-                if workspace is None and workspace_bytes:
-                    workspace = torch.empty(workspace_bytes + 256, dtype=torch.uint8, device=self.device)
-                return call(*(_ws(workspace) if workspace is not None else (None, 0)), _stream())
+            with torch.cuda.stream(stream):                       # None: the device's current one
+                return call(*args, **kw)
+
+    def _scratch(self, n: int, workspace: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int, int]:
+        if workspace is None:
+            workspace = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
+        return (workspace, *_ws(workspace))
 
     # -- pages -----------------------------------------------------------------------------------------------------------------
 
@@ -705,72 +717,88 @@ class PagedCache:
         """New rows [n_layers, T, Hkv, hd] to the end of their sequences: all of them, or with mask [T, words] and node [n_seqs] (for
         instance result[:, 0] of n_seqs walks) those on the path to each sequence's accepted node; node -1 appends nothing.
         status [n_seqs] int32 receives PAGES_*."""
-        if rows_k.dim() != 4 or rows_k.shape != rows_v.shape or rows_k.shape[0] != self.n_layers or rows_k.stride() != rows_v.stride():
+        shape, strides = rows_k.shape, rows_k.stride()
+        if len(shape) != 4 or rows_v.shape != shape or shape[0] != self.n_layers or rows_v.stride() != strides:
             raise ValueError("rows_k and rows_v are [n_layers, T, Hkv, hd] of the same strides")
-        T, words = rows_k.shape[1], 0
-        self._ints(row_start, self.n_seqs + 1)
-        if T == 0:
-            return
-        stride = self._rows(rows_k[0], self.cfg.n_kv_heads)
-        self._rows(rows_v[0], self.cfg.n_kv_heads)
+        T, L, Hkv = shape[1], self.n_layers, self.cfg.n_kv_heads
+        rp, sp = self._ints(row_start, self.n_seqs + 1), self._ints(status, self.n_seqs)
+        stride = self._rows(rows_k[0], Hkv, T)
+        self._rows(rows_v[0], Hkv, T)
         mp, words = self._mask(mask, T)
         if node is not None and (node.dtype != torch.int32 or node.device != self.device or tuple(node.shape) != (self.n_seqs,)):
             raise ValueError("node is [n_seqs] int32")
-        node_stride = 1 if node is None or self.n_seqs == 1 else node.stride(0)
-        step = rows_k.stride(0) * rows_k.element_size()
-        kp = (C.c_void_p * self.n_layers)(*[rows_k.data_ptr() + l * step for l in range(self.n_layers)])
-        vp = (C.c_void_p * self.n_layers)(*[rows_v.data_ptr() + l * step for l in range(self.n_layers)])
-        self._call(self._pages_ws, workspace, stream, lambda wp, wn, st: _check(lib.spiffy_pages_append(
-            self._cfg, self._cache, self.n_layers, self._layers, kp, vp, stride, _ptr(row_start), T, mp, words,
-            None if node is None else node.data_ptr(), node_stride, self._ints(status, self.n_seqs), wp, wn, st), "spiffy_pages_append"))
+        if T == 0:
+            return
+        if self._elsewhere(stream):
+            return self._there(stream, self.append, rows_k, rows_v, row_start, mask, node, status, workspace)
+        step, k0, v0 = strides[0] * rows_k.element_size(), rows_k.data_ptr(), rows_v.data_ptr()
+        kp = (C.c_void_p * L)(*range(k0, k0 + L * step, step)) if step else (C.c_void_p * L)(*[k0] * L)
+        vp = (C.c_void_p * L)(*range(v0, v0 + L * step, step)) if step else (C.c_void_p * L)(*[v0] * L)
+        ws, wp, wn = self._scratch(self._pages_ws, workspace)
+        _check(lib.spiffy_pages_append(self._cfg, self._cache, L, self._layers, kp, vp, stride, rp, T, mp, words,
+                                       None if node is None else node.data_ptr(), 1 if node is None or self.n_seqs == 1 else node.stride(0),
+                                       sp, wp, wn, self._current()), "spiffy_pages_append")
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
              stream=None) -> None:
-        """Empty sequences dst [n] become copies of sequences src [n] (int32): full pages are shared, a last one that is not full is copied."""
-        n = src.shape[0]
-        sp, dp, tp = self._ints(src), self._ints(dst, n), self._ints(status, n)
-        if n:
-            self._call(self._pages_ws, workspace, stream, lambda wp, wn, st: _check(lib.spiffy_pages_fork(
-                self._cfg, self._cache, self.n_layers, self._layers, sp, dp, n, tp, wp, wn, st), "spiffy_pages_fork"))
+        """Empty sequences dst [n] become copies of sequences src [n] (int32): full pages are shared, a last one that is not full is copied.
+        status [n] int32 receives PAGES_*."""
+        n = src.shape[0] if src.dim() else -1
+        sp, dp, tp = self._ints(src, n), self._ints(dst, n), self._ints(status, n)
+        if n == 0:
+            return
+        if self._elsewhere(stream):
+            return self._there(stream, self.fork, src, dst, status, workspace)
+        ws, wp, wn = self._scratch(self._pages_ws, workspace)
+        _check(lib.spiffy_pages_fork(self._cfg, self._cache, self.n_layers, self._layers, sp, dp, n, tp, wp, wn, self._current()), "spiffy_pages_fork")
 
     def free(self, seqs: torch.Tensor, stream=None) -> None:
         """Sequences seqs [n] (int32) become empty, their pages lose a reference."""
-        sp = self._ints(seqs)
-        if seqs.shape[0]:
-            self._call(0, None, stream, lambda wp, wn, st: _check(lib.spiffy_pages_free(self._cache, sp, seqs.shape[0], st), "spiffy_pages_free"))
+        n = seqs.shape[0] if seqs.dim() else -1
+        sp = self._ints(seqs, n)
+        if n == 0:
+            return
+        if self._elsewhere(stream):
+            return self._there(stream, self.free, seqs)
+        _check(lib.spiffy_pages_free(self._cache, sp, n, self._current()), "spiffy_pages_free")
 
     def compact(self, n_used: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The pages in use move to the lowest ids; returns how many they are, [1] int32."""
-        def call(wp, wn, st):
-            out = torch.empty(1, dtype=torch.int32, device=self.device) if n_used is None else n_used
-            _check(lib.spiffy_pages_compact(self._cfg, self._cache, self.n_layers, self._layers, self._ints(out, 1), wp, wn, st),
-                   "spiffy_pages_compact")
-            return out
-        return self._call(self._pages_ws, workspace, stream, call)
+        if self._elsewhere(stream):
+            return self._there(stream, self.compact, n_used, workspace)
+        if n_used is None:
+            n_used = torch.empty(1, dtype=torch.int32, device=self.device)
+        up = self._ints(n_used, 1)
+        ws, wp, wn = self._scratch(self._pages_ws, workspace)
+        _check(lib.spiffy_pages_compact(self._cfg, self._cache, self.n_layers, self._layers, up, wp, wn, self._current()), "spiffy_pages_compact")
+        return n_used
 
     # -- attention -------------------------------------------------------------------------------------------------------------
 
     def summarize(self, start: Optional[torch.Tensor] = None, stream=None) -> None:
         """Brings `summary` up to date for the pages that hold rows start[s] .. len[s]-1 (None: all rows)."""
         sp = self._ints(start, self.n_seqs)
-        self._call(0, None, stream, lambda wp, wn, st: _check(lib.spiffy_page_summary(self._cfg, self._cache, self.n_layers, self._layers, sp, st),
-                                                             "spiffy_page_summary"))
+        if self._elsewhere(stream):
+            return self._there(stream, self.summarize, start)
+        _check(lib.spiffy_page_summary(self._cfg, self._cache, self.n_layers, self._layers, sp, self._current()), "spiffy_page_summary")
 
     def select(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int, n_sel: int, keep_first: int = 0, keep_last: int = 1,
                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The n_sel pages of every (sequence, kv head) whose summaries promise the highest scores with the new rows' queries q
-        [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; its first keep_first and last keep_last pages come before all others."""
-        lp, stride, rp = self._layer(layer), self._rows(q, self.cfg.n_q_heads), self._ints(row_start, self.n_seqs + 1)
-        shape = (self.n_seqs, self.cfg.n_kv_heads, n_sel)
+        [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; a sequence's first keep_first and last keep_last pages come before all others."""
+        T, shape = q.shape[0], (self.n_seqs, self.cfg.n_kv_heads, n_sel)
+        lp, stride, rp = self._layer(layer), self._rows(q, self.cfg.n_q_heads, T), self._ints(row_start, self.n_seqs + 1)
         if out is not None and tuple(out.shape) != shape:
             raise ValueError("out is %s" % (shape,))
-
-        def call(wp, wn, st):
-            o = torch.empty(shape, dtype=torch.int32, device=self.device) if out is None else out
-            _check(lib.spiffy_page_select(self._cfg, self._cache, lp, q.data_ptr(), stride, rp, q.shape[0], max_rows, n_sel, keep_first,
-                                          keep_last, self._typed(o, torch.int32), wp, wn, st), "spiffy_page_select")
-            return o
-        return self._call(self._select_ws, workspace, stream, call)
+        if self._elsewhere(stream):
+            return self._there(stream, self.select, layer, q, row_start, max_rows, n_sel, keep_first, keep_last, out, workspace)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        op = self._typed(out, torch.int32)
+        ws, wp, wn = self._scratch(self._select_ws, workspace)
+        _check(lib.spiffy_page_select(self._cfg, self._cache, lp, q.data_ptr(), stride, rp, T, max_rows, n_sel, keep_first, keep_last, op,
+                                      wp, wn, self._current()), "spiffy_page_select")
+        return out
 
     def attend_workspace_bytes(self, max_rows: int) -> int:
         n = self._attn_ws.get(max_rows)
@@ -787,25 +815,24 @@ class PagedCache:
         """Attention of the new rows q [T, Hq, hd] over their sequences' cache rows and over the new rows k, v [T, Hkv, hd] that mask
         [T, words] names (None: all of the sequence); rows may be strided views of one q | k | v buffer.  selected: only these pages of
         the cache (see select).  Returns [T, Hq, hd]; rows behind row_start[-1] are not written."""
-        Hq, Hkv, T = self.cfg.n_q_heads, self.cfg.n_kv_heads, q.shape[0]
-        lp, qs, ks, vs = self._layer(layer), self._rows(q, Hq), self._rows(k, Hkv, T), self._rows(v, Hkv, T)
+        Hq, Hkv, hd, T = self.cfg.n_q_heads, self.cfg.n_kv_heads, self.cfg.head_dim, q.shape[0]
+        lp, qs, ks, vs = self._layer(layer), self._rows(q, Hq, T), self._rows(k, Hkv, T), self._rows(v, Hkv, T)
         if ks != vs:
             raise ValueError("rows of k and v have the same stride")
-        rp, (mp, words), n_sel, os_ = self._ints(row_start, self.n_seqs + 1), self._mask(mask, T), 0, Hq * self.cfg.head_dim
+        rp, (mp, words), selp, n_sel = self._ints(row_start, self.n_seqs + 1), self._mask(mask, T), None, 0
         if selected is not None:
             if selected.dim() != 3 or tuple(selected.shape[:2]) != (self.n_seqs, Hkv):
                 raise ValueError("selected is [n_seqs, Hkv, n_sel]")
-            n_sel = selected.shape[2]
-        selp = None if selected is None else self._typed(selected, torch.int32)
-        if out is not None:
-            os_ = self._rows(out, Hq, T)
+            selp, n_sel = self._typed(selected, torch.int32), selected.shape[2]
+        os_ = Hq * hd if out is None else self._rows(out, Hq, T)
         if T == 0:
             return torch.empty_like(q) if out is None else out
-
-        def call(wp, wn, st):
-            o = torch.empty((T, Hq, self.cfg.head_dim), dtype=self._dt, device=self.device) if out is None else out
-            _check(lib.spiffy_tree_attention(self._cfg, self._cache, lp, q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks, rp, T, max_rows,
-                                             mp, words, selp, n_sel, self.cfg.head_dim ** -0.5 if scale is None else scale, o.data_ptr(), os_,
-                                             wp, wn, st), "spiffy_tree_attention")
-            return o
-        return self._call(self.attend_workspace_bytes(max_rows), workspace, stream, call)
+        if self._elsewhere(stream):
+            return self._there(stream, self.attend, layer, q, k, v, row_start, max_rows, mask, selected, scale, out, workspace)
+        if out is None:
+            out = torch.empty((T, Hq, hd), dtype=self._dt, device=self.device)
+        ws, wp, wn = self._scratch(self.attend_workspace_bytes(max_rows), workspace)
+        _check(lib.spiffy_tree_attention(self._cfg, self._cache, lp, q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks, rp, T, max_rows, mp, words,
+                                         selp, n_sel, hd ** -0.5 if scale is None else scale, out.data_ptr(), os_, wp, wn, self._current()),
+               "spiffy_tree_attention")
+        return out
