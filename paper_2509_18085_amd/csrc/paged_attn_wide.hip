@@ -150,8 +150,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       for (int n = 0; n < NN; ++n)
         o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(v_half(buf, i, n, 0), v_half(buf, i, n, 1)), x[i], o[n], 0, 0, 0);
   };
-  // Step t of the pipeline, BUF = t % 2: scores `next` of tile t + 1 between the exponentials of s
-  auto step = [&](auto BUF, f32x16& s, f32x16& next) {
+  // Step t of the pipeline, BUF = t % 2: scores `next` of tile t + 1 between the exponentials of s.  fetch(i), i = 0 .. 7: loads that start
+  // on the way; all of them at once would hold every wavefront up until the CU's 64 bytes a clock have let them through
+  auto step = [&](auto BUF, f32x16& s, f32x16& next, auto fetch) {
     constexpr int buf = decltype(BUF)::value;
     bf16x8 k[NK], x[2];
     bf16x4 v[2][NN][2];
@@ -169,6 +170,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
         v[i / NN][i % NN][0] = v_half(buf, i / NN, i % NN, 0);
         v[i / NN][i % NN][1] = v_half(buf, i / NN, i % NN, 1);
       }
+      fetch(i);
     }
     // issue order: a matrix instruction, two exponentials with what is around them, two reads of values
 #pragma unroll
@@ -177,6 +179,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
       if (i < 2 * NN) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      if (QUAD && i % 2 == 1) __builtin_amdgcn_sched_group_barrier(0x020, RPT / 2 ? RPT / 2 : 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
     }
 #pragma unroll
@@ -244,10 +247,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
         }
       }
     };
+    auto piece_of = [&](const bf16_t* pool, long long row) { return *reinterpret_cast<const u32x4*>(pool + row + lane_at); };
     auto load = [&](const bf16_t* pool, u32x4 (&x)[RPT]) {
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
-        if constexpr (QUAD) x[i] = *reinterpret_cast<const u32x4*>(pool + at[i] + lane_at);
+        if constexpr (QUAD) x[i] = piece_of(pool, at[i]);
         else x[i] = at[i] >= 0 ? *reinterpret_cast<const u32x4*>(pool + at[i]) : u32x4{};
       }
     };
@@ -305,15 +309,32 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
         clear(t + 1, vx);
         put_values(1 - buf);
       }
-      if (t + 2 < tiles) load(pv, vx);
-      if (t + 3 < tiles) {
+      if constexpr (QUAD) {                               // behind the last tile its rows come again, and nobody reads them
+        long long at_v[RPT];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) at_v[i] = at[i];
         look_up(t + 3);
-        load(pk, kx);
         look_ahead(t + 4);
+        if (!busy) {
+#pragma unroll
+          for (int i = 0; i < RPT; ++i) vx[i] = piece_of(pv, at_v[i]), kx[i] = piece_of(pk, at[i]);
+          return;
+        }
+        if (batch + (t + 1) * kTile > bad) hide(s, __ballot(find(batch + t * kTile + lane) >= 0));
+        step(BUF, s, next, [&](int i) {                   // `next` behind the last tile: scores of what LDS holds, and nothing reads them
+          if (i % 2 == 1 && i / 2 < RPT) vx[i / 2] = piece_of(pv, at_v[i / 2]);
+          if (i % 2 == 1 && i / 2 >= 4 - RPT) kx[i / 2 - (4 - RPT)] = piece_of(pk, at[i / 2 - (4 - RPT)]);
+        });
+      } else {
+        if (t + 2 < tiles) load(pv, vx);
+        if (t + 3 < tiles) {
+          look_up(t + 3);
+          load(pk, kx);
+        }
+        if (!busy) return;
+        if (batch + (t + 1) * kTile > bad) hide(s, __ballot(find(batch + t * kTile + lane) >= 0));
+        step(BUF, s, next, [](int) {});
       }
-      if (!busy) return;
-      if (batch + (t + 1) * kTile > bad) hide(s, __ballot(find(batch + t * kTile + lane) >= 0));
-      step(BUF, s, next);                                 // behind the last tile `next` are scores of what LDS holds; nothing reads them
     };
     for (int t = 0; t < tiles; t += 2) {
       turn(t, std::integral_constant<int, 0>{}, sa, sb);
