@@ -32,7 +32,7 @@ typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_ptr_t;
 // QUAD: head_dim == HDP, pages of a multiple of the four (64 channels: eight) rows of a wavefront's load lie in one page, their place is the same for all
 // lanes but for a constant.
 template <int HDP, bool QUAD>
-__global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnArgs a, const AttnWs ws, int want, int row_tiles, int log_ps) {
+__global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnArgs a, const AttnWs ws, int want, int row_tiles, unsigned magic) {
   constexpr int ROWS = kWideRows;
   constexpr int NK = HDP / 16, NN = HDP / 32;             // steps of the first product, 32-channel tiles of the second
   constexpr int PIECES = HDP / 8, RPT = kTile * PIECES / kThreads;      // 16-byte pieces of a row; rows of a thread
@@ -179,7 +179,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
       if (i < 2 * NN) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      if (QUAD && i % 2 == 1) __builtin_amdgcn_sched_group_barrier(0x020, RPT / 2 ? RPT / 2 : 1, 0);
+      if (QUAD && i % 2 == 1 && i / 2 < 2 * RPT) {
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      }
       __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
     }
 #pragma unroll
@@ -197,7 +200,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   const int batch_keys = (int)min((long long)(kWideEntries - 2) * ps, (long long)kWideKeys);
   for (int batch = lo; batch < cache_hi; batch += batch_keys) {
     const int end = min(cache_hi, batch + batch_keys);
-    auto entry = [&](int key) { return log_ps >= 0 ? key >> log_ps : (int)((unsigned)key / (unsigned)ps); };
+    auto entry = [&](int key) {                           // key / ps: the product is at most one too low
+      const int e = (int)__umulhi((unsigned)key, magic);
+      return key - e * ps >= ps ? e + 1 : e;
+    };
     const int e0 = entry(batch), e1 = entry(end - 1);
     __syncthreads();
     if (tid == 0) s_bad = end;
@@ -210,7 +216,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
         id = c.table[(long long)u.s * c.max_pages + slot];
         rows = id >= 0 && id < c.n_pages ? clamp_int(len - slot * ps, 0, ps) : 0;
       }
-      s_page[e - e0] = make_int2(id, rows);
+      // page and kv head (QUAD: their number, which fits 32 bits, since 2^32 times four rows of 128 bytes are more than there is memory)
+      s_page[e - e0] = make_int2(QUAD ? (rows ? id * a.h.Hkv : 0) + kvh : id, rows);
       if (rows < ps) atomicMin(&s_bad, e * ps + rows);
     }
     __syncthreads();
@@ -219,28 +226,31 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     auto find = [&](int key) {
       const int e = entry(min(key, end - 1)), off = min(key, end - 1) - e * ps;
       const int2 p = s_page[e - e0];
-      return key < end && off < p.y ? p.x * row_of_page + (long long)kvh * ps + off : -1ll;
+      return key < end && off < p.y ? p.x * row_of_page + (long long)kvh * ps + off : -1ll;      // QUAD: only whether there is one
     };
     // Where this thread's rows of tile t lie.  QUAD: rows of one wavefront, the first of them; otherwise each lane's piece, -1: none.
     long long at[RPT];
     u32x4 kx[RPT], vx[RPT];
     const int lane_at = (my_row & (WROWS - 1)) * HDP + my_piece * 8;
     // QUAD: the list's entry is read a step before it is used
-    int2 page[RPT];
+    int page[RPT], off[RPT];
     auto quad_key = [&](int t, int i) {                   // batches begin at multiples of WROWS
       return min(batch + t * kTile + __builtin_amdgcn_readfirstlane(my_row) + i * RSTEP, end - 1) & -WROWS;
     };
     auto look_ahead = [&](int t) {
       if constexpr (QUAD)
 #pragma unroll
-        for (int i = 0; i < RPT; ++i) page[i] = s_page[entry(quad_key(t, i)) - e0];
+        for (int i = 0; i < RPT; ++i) {
+          const int key = quad_key(t, i), e = entry(key);
+          page[i] = s_page[e - e0].x;
+          off[i] = key - e * ps;
+        }
     };
     auto look_up = [&](int t) {
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
         if constexpr (QUAD) {
-          const int key = quad_key(t, i), id = __builtin_amdgcn_readfirstlane(page[i].y > 0 ? page[i].x : 0);
-          at[i] = (id * row_of_page + (long long)kvh * ps + (key - entry(key) * ps)) * HDP;
+          at[i] = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane(page[i]) * (unsigned)(ps * HDP)) + off[i] * HDP;
         } else {
           const long long r = find(batch + t * kTile + my_row + i * RSTEP);
           at[i] = r >= 0 && my_piece * 8 < hd ? r * hd + my_piece * 8 : -1;
@@ -301,31 +311,37 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     auto turn = [&](int t, auto BUF, f32x16& s, f32x16& next) {
       constexpr int buf = decltype(BUF)::value;
       __syncthreads();
-      if (t + 2 < tiles) {
-        clear(t + 2, kx);
-        put_keys(buf);
-      }
-      if (t + 1 < tiles) {
-        clear(t + 1, vx);
-        put_values(1 - buf);
-      }
-      if constexpr (QUAD) {                               // behind the last tile its rows come again, and nobody reads them
+      if constexpr (QUAD) {
+        // A thread's values of tile t + 1 and keys of tile t + 2, loaded during the last step, go to LDS during this one, each just before the
+        // load that takes its registers.  Behind the last tile its rows come again, and nobody reads them.
         long long at_v[RPT];
 #pragma unroll
         for (int i = 0; i < RPT; ++i) at_v[i] = at[i];
         look_up(t + 3);
         look_ahead(t + 4);
+        clear(t + 2, kx);
+        clear(t + 1, vx);
+        auto fetch = [&](int i) {
+          if (i < RPT) {
+            *reinterpret_cast<u32x4*>(s_kv + (3 - buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = vx[i];
+            vx[i] = piece_of(pv, at_v[i]);
+          } else if (i < 2 * RPT) {
+            *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + (i - RPT) * RSTEP, my_piece)) = kx[i - RPT];
+            kx[i - RPT] = piece_of(pk, at[i - RPT]);
+          }
+        };
         if (!busy) {
 #pragma unroll
-          for (int i = 0; i < RPT; ++i) vx[i] = piece_of(pv, at_v[i]), kx[i] = piece_of(pk, at[i]);
+          for (int i = 0; i < 2 * RPT; ++i) fetch(i);
           return;
         }
         if (batch + (t + 1) * kTile > bad) hide(s, __ballot(find(batch + t * kTile + lane) >= 0));
         step(BUF, s, next, [&](int i) {                   // `next` behind the last tile: scores of what LDS holds, and nothing reads them
-          if (i % 2 == 1 && i / 2 < RPT) vx[i / 2] = piece_of(pv, at_v[i / 2]);
-          if (i % 2 == 1 && i / 2 >= 4 - RPT) kx[i / 2 - (4 - RPT)] = piece_of(pk, at[i / 2 - (4 - RPT)]);
+          if (i % 2 == 1) fetch(i / 2);
         });
       } else {
+        if (t + 2 < tiles) put_keys(buf);
+        if (t + 1 < tiles) put_values(1 - buf);
         if (t + 2 < tiles) load(pv, vx);
         if (t + 3 < tiles) {
           look_up(t + 3);
@@ -470,13 +486,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 }  // namespace
 
 hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st) {
-  const int ps = a.c.page_size, log_ps = ps & (ps - 1) ? -1 : __builtin_ctz(ps);
+  const int ps = a.c.page_size;
+  const unsigned magic = 0xffffffffu / (unsigned)ps;
   const unsigned grid = (unsigned)(((long long)want + a.c.n_seqs) * a.h.Hkv * row_tiles);
   const bool quad = ps % (a.h.hd == 64 ? 8 : 4) == 0;
-  if (a.h.hd == 128 && quad) tree_wide_kernel<128, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
-  else if (a.h.hd == 64 && quad) tree_wide_kernel<64, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
-  else if (a.h.hd > 64) tree_wide_kernel<128, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
-  else tree_wide_kernel<64, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, log_ps);
+  if (a.h.hd == 128 && quad) tree_wide_kernel<128, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);
+  else if (a.h.hd == 64 && quad) tree_wide_kernel<64, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);
+  else if (a.h.hd > 64) tree_wide_kernel<128, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);
+  else tree_wide_kernel<64, false><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);
   return hipGetLastError();
 }
 
