@@ -96,7 +96,8 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   }
 
   // the tree's bits of this workgroup's rows
-  if (hi > u.tree0) {
+  auto fill_bits = [&]() {
+    if (hi <= u.tree0) return;
     const int words = (u.rows.n + 63) >> 6;
     for (int i = tid; i < words * RT * 16; i += 256) {
       const int r = i % (RT * 16), w = i / (RT * 16);
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
       if (a.rows.mask) b &= w < a.rows.words ? a.rows.mask[(long long)(u.rows.first + row) * a.rows.words + w] : 0;
       bits[i] = b;
     }
-  }
+  };
 
   float m[RT], l[RT];
   f32x4 o[RT][NP][VW];
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   for (int batch = lo; batch < cache_hi; batch += BATCH) {
     const int end = min(cache_hi, batch + BATCH);
     const int e0 = FAST ? batch >> log_ps : batch / ps, e1 = FAST ? (end - 1) >> log_ps : (end - 1) / ps;
-    __syncthreads();
+    if (batch > lo) __syncthreads();
     const int len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += 256) {
       const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
@@ -228,6 +229,7 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
       page_id[e - e0] = rows ? id : 0;
       page_rows[e - e0] = rows;
     }
+    if (batch == lo) fill_bits();                         // with the first list: their loads wait together
     __syncthreads();
     if constexpr (FAST) {
       int have[NT];                                       // rows of the tiles; they and where the tiles lie are the same in all lanes
@@ -323,6 +325,7 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   }
 
   // ---- the new rows
+  if (cache_hi <= lo) fill_bits();
   __syncthreads();
   for (int at = max(lo - u.tree0, 0) + wave * STEP; at < hi - u.tree0; at += 4 * STEP) {
     unsigned seen[RT], any = 0;                           // bit x: the row of this lane's column attends to new row at + x
@@ -565,7 +568,7 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   // no sequence can have more than one unit: nothing to join
   const long long cache = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size;
-  if ((cache + kAlign - 1) / kAlign + a.max_rows / kAlign <= kMinBlocks) return hipSuccess;
+  if (s.want == 1 || (cache + kAlign - 1) / kAlign + a.max_rows / kAlign <= kMinBlocks) return hipSuccess;
   // few rows have many partial results each and wait for them: four wavefronts a row; many rows: one
   const dim3 grid(a.rows.T, a.h.Hq);
   const int threads = (long long)a.rows.T * a.h.Hq <= 2048 ? 256 : 64;

@@ -38,9 +38,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   constexpr int PIECES = HDP / 8, RPT = kTile * PIECES / kThreads;      // 16-byte pieces of a row; rows of a thread
   constexpr int RSTEP = kThreads / PIECES, WROWS = kWave / PIECES;      // rows of all threads, of a wavefront
   constexpr int ROWB = HDP * 2, TILEB = kTile * ROWB;
-  // K tiles 0, 1, V tiles 0, 1; before the new rows the page list, behind it their bits
-  __shared__ __align__(16) unsigned char s_kv[4 * TILEB];
+  __shared__ __align__(16) unsigned char s_kv[4 * TILEB];               // K tiles 0, 1, V tiles 0, 1
   __shared__ __align__(16) int2 s_page[kWideEntries];     // page, rows in it
+  __shared__ uint64_t bits[(SPIFFY_MAX_TREE / 64) * ROWS];              // [words][ROWS]: what the rows attend to
   __shared__ unsigned long long s_any[SPIFFY_MAX_TREE / 64];
   __shared__ int s_bad;                                   // the first key of a batch that has no row
   __shared__ unsigned s_odd[kTile / 32];                  // new rows of a tile whose values are not all finite
@@ -191,6 +191,18 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       for (int n = 0; n < NN; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(v[i][n][0], v[i][n][1]), x[i], o[n], 0, 0, 0);
   };
 
+  auto fill_bits = [&]() {
+    if (hi <= u.tree0) return;
+    const int words = (u.rows.n + 63) >> 6;
+    for (int i = tid; i < words * ROWS; i += kThreads) {
+      const int r = i % ROWS, w = i / ROWS, left = u.rows.n - 64 * w;
+      uint64_t b = r0 + r < R ? (left < 64 ? (1ull << left) - 1 : ~0ull) : 0;
+      if (a.rows.mask && b) b &= w < a.rows.words ? a.rows.mask[(long long)(u.rows.first + (r0 + r) / g) * a.rows.words + w] : 0;
+      bits[i] = b;
+      if (b) atomicOr(&s_any[w], (unsigned long long)b);
+    }
+  };
+
   // ---- the cache
   const int my_row = tid / PIECES, my_piece = tid % PIECES;
   const bf16_t* pk = reinterpret_cast<const bf16_t*>(a.pk);
@@ -207,6 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     const int e0 = entry(batch), e1 = entry(end - 1);
     __syncthreads();
     if (tid == 0) s_bad = end;
+    if (batch == lo && tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
     __syncthreads();
     const int len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += kThreads) {
@@ -220,6 +233,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       s_page[e - e0] = make_int2(QUAD ? (rows ? id * a.h.Hkv : 0) + kvh : id, rows);
       if (rows < ps) atomicMin(&s_bad, e * ps + rows);
     }
+    if (batch == lo) fill_bits();                         // with the first list: their loads wait together
     __syncthreads();
     const int tiles = (end - batch + kTile - 1) / kTile, bad = s_bad;      // below `bad` every key has a row
     // row of the pool that holds a key, -1: none
@@ -272,37 +286,37 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       for (int i = 0; i < RPT; ++i)
         if (find(batch + t * kTile + my_row + i * RSTEP) < 0) x[i] = u32x4{};
     };
-    auto put_keys = [&](int buf) {
+    auto put_keys = [&](int buf, const u32x4 (&x)[RPT]) {
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + i * RSTEP, my_piece)) = kx[i];
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + buf * TILEB + k_at(my_row + i * RSTEP, my_piece)) = x[i];
     };
-    auto put_values = [&](int buf) {
+    auto put_values = [&](int buf, const u32x4 (&x)[RPT]) {
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + (2 + buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = vx[i];
+      for (int i = 0; i < RPT; ++i) *reinterpret_cast<u32x4*>(s_kv + (2 + buf) * TILEB + v_at(my_row + i * RSTEP, my_piece)) = x[i];
     };
-    // tile 0 and the keys of tile 1 into LDS; the keys of tile 2 and the values of tile 1 on their way
-    look_ahead(0);
-    look_up(0);
-    load(pk, kx);
-    load(pv, vx);
-    clear(0, kx);
-    clear(0, vx);
-    put_keys(0);
-    put_values(0);
-    if (tiles > 1) {
+    // tile 0 and the keys of tile 1 into LDS, the keys of tile 2 and the values of tile 1 on their way: all of them start together (behind
+    // the last tile its rows come again)
+    {
+      u32x4 k0[RPT], v0[RPT], k1[RPT];
+      look_ahead(0);
+      look_up(0);
+      load(pk, k0);
+      load(pv, v0);
       look_ahead(1);
       look_up(1);
-      load(pk, kx);
+      load(pk, k1);
       load(pv, vx);
-      clear(1, kx);
-      put_keys(1);
-    }
-    if (tiles > 2) {
       look_ahead(2);
       look_up(2);
       load(pk, kx);
+      look_ahead(3);
+      clear(0, k0);
+      clear(0, v0);
+      clear(1, k1);
+      put_keys(0, k0);
+      put_values(0, v0);
+      put_keys(1, k1);
     }
-    look_ahead(3);
     __syncthreads();
     f32x16 sa, sb;
     if (busy) scores(0, sa);
@@ -340,8 +354,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
           if (i % 2 == 1) fetch(i / 2);
         });
       } else {
-        if (t + 2 < tiles) put_keys(buf);
-        if (t + 1 < tiles) put_values(1 - buf);
+        if (t + 2 < tiles) put_keys(buf, kx);
+        if (t + 1 < tiles) put_values(1 - buf, vx);
         if (t + 2 < tiles) load(pv, vx);
         if (t + 3 < tiles) {
           look_up(t + 3);
@@ -360,18 +374,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 
   // ---- the new rows
   if (hi > u.tree0) {
-    uint64_t* bits = reinterpret_cast<uint64_t*>(s_page); // [words][ROWS]
-    static_assert(sizeof(s_page) >= sizeof(uint64_t) * ROWS * (SPIFFY_MAX_TREE / 64), "the bits take the page list's place");
-    const int words = (u.rows.n + 63) >> 6;
-    __syncthreads();
-    if (tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < words * ROWS; i += kThreads) {
-      const int r = i % ROWS, w = i / ROWS, left = u.rows.n - 64 * w;
-      uint64_t b = r0 + r < R ? (left < 64 ? (1ull << left) - 1 : ~0ull) : 0;
-      if (a.rows.mask && b) b &= w < a.rows.words ? a.rows.mask[(long long)(u.rows.first + (r0 + r) / g) * a.rows.words + w] : 0;
-      bits[i] = b;
-      if (b) atomicOr(&s_any[w], (unsigned long long)b);
+    if (cache_hi <= lo) {
+      if (tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
+      __syncthreads();
+      fill_bits();
     }
     __syncthreads();
     const long long first = u.rows.first;
