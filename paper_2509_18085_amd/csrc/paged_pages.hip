@@ -161,11 +161,11 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(const PagesAr
   }
 }
 
-// A wavefront a (row, layer): 16 bytes a lane, head by head into the page.
-__global__ __launch_bounds__(256) void append_rows_kernel(const PagesArgs a) {
+// A wavefront a row and `layers` layers: 16 bytes a lane, head by head into the page.
+__global__ __launch_bounds__(256) void append_rows_kernel(const PagesArgs a, int layers) {
   const PagedView& c = a.c;
   const int lane = threadIdx.x & 63, ps = c.page_size;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), layer = blockIdx.y;
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= a.rows.T) return;
   const int s = seq_of_row(a.rows, c.n_seqs, t);
   if (s >= c.n_seqs) return;
@@ -185,15 +185,18 @@ __global__ __launch_bounds__(256) void append_rows_kernel(const PagesArgs a) {
   const int page = slot < c.max_pages ? c.table[(long long)s * c.max_pages + slot] : -1;
   if (page < 0 || page >= c.n_pages) return;
   const int es = a.h.f32 ? 4 : 2, seg = a.h.hd * es / 16;       // 16-byte pieces of a head's row
-  const u32x4* k = reinterpret_cast<const u32x4*>((const char*)a.row_layers.k[layer] + (long long)t * a.row_stride * es);
-  const u32x4* v = reinterpret_cast<const u32x4*>((const char*)a.row_layers.v[layer] + (long long)t * a.row_stride * es);
-  u32x4* pk = reinterpret_cast<u32x4*>(a.layers.k[layer]);
-  u32x4* pv = reinterpret_cast<u32x4*>(a.layers.v[layer]);
+  const long long from = (long long)t * a.row_stride * es;
+  const int last = min((int)(blockIdx.y + 1) * layers, a.layers.n);
   for (int x = lane; x < a.h.Hkv * seg; x += kWave) {
     const int h = x / seg;
     const long long to = (((long long)page * a.h.Hkv + h) * ps + off) * seg + (x - h * seg);
-    pk[to] = k[x];
-    pv[to] = v[x];
+#pragma unroll 4
+    for (int l = blockIdx.y * layers; l < last; ++l) {
+      const u32x4 k = reinterpret_cast<const u32x4*>((const char*)a.row_layers.k[l] + from)[x];
+      const u32x4 v = reinterpret_cast<const u32x4*>((const char*)a.row_layers.v[l] + from)[x];
+      reinterpret_cast<u32x4*>(a.layers.k[l])[to] = k;
+      reinterpret_cast<u32x4*>(a.layers.v[l])[to] = v;
+    }
   }
 }
 
@@ -388,7 +391,10 @@ hipError_t launch_append_plan(const PagesArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_append_rows(const PagesArgs& a, hipStream_t st) {
-  append_rows_kernel<<<dim3(cdiv(a.rows.T, 4), a.layers.n), 256, 0, st>>>(a);
+  // layers of a wavefront: as many as leave 8192 of them, since most rows of a tree are not on its path and a wavefront only finds that out
+  const long long jobs = (long long)a.rows.T * a.layers.n;
+  const int layers = jobs <= 8192 ? 1 : (jobs / 8192 < a.layers.n ? (int)(jobs / 8192) : a.layers.n);
+  append_rows_kernel<<<dim3(cdiv(a.rows.T, 4), cdiv(a.layers.n, layers)), 256, 0, st>>>(a, layers);
   return hipGetLastError();
 }
 hipError_t launch_fork_plan(const PagesArgs& a, hipStream_t st) {

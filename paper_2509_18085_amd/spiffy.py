@@ -599,7 +599,7 @@ def tree_mask(edges, n: int, device="cuda") -> torch.Tensor:
             raise ValueError("an edge goes from a node to a later one: got (%d, %d) of %d nodes" % (p, c, n))
         rows[c] |= rows[p]
     words = [[r >> 64 * w & (1 << 64) - 1 for w in range((n + 63) // 64)] for r in rows]
-    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in words], dtype=torch.int64, device=device)
+    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in words], dtype=torch.int64, device=device).reshape(n, (n + 63) // 64)
 
 
 # the current stream's handle without the Python object around it (some 3 us a call), where torch has it
@@ -614,7 +614,8 @@ class PagedCache:
     (optional) [n_layers, n_pages, Hkv, 2, hd]: contiguous tensors on one device, kept as they are.  `empty` makes them.  New rows
     of all sequences lie one behind the other, row_start [n_seqs + 1] int32 says where those of each begin; max_rows is a bound on
     the new rows of one sequence.  Nothing waits for the device.  Outputs and workspaces that the caller does not pass are
-    allocated by the call, so calls that only read the cache may run at the same time on several streams."""
+    allocated by the call, so calls that only read the cache may run at the same time on several streams; a workspace that the
+    caller passes serves one call at a time (two graphs that were captured with the same one must not run at once)."""
 
     def __init__(self, cfg: ModelCfg, k: torch.Tensor, v: torch.Tensor, refs: torch.Tensor, table: torch.Tensor, len: torch.Tensor,
                  summary: Optional[torch.Tensor] = None):
@@ -638,6 +639,7 @@ class PagedCache:
                                                              for l in range(self.n_layers)])
         self._cfg, self._cache = C.byref(self.cfg), C.byref(self._struct)
         self._layer_refs = [C.byref(x) for x in self._layers]
+        self._ptrs = C.c_void_p * max(1, self.n_layers)
         self._pages_ws = int(lib.spiffy_pages_workspace_bytes(self._cache))
         self._select_ws = int(lib.spiffy_page_select_workspace_bytes(self._cfg, self._cache))
         if not self._pages_ws or not self._select_ws:
@@ -685,12 +687,18 @@ class PagedCache:
             raise ValueError("mask is [T, words] int64")
         return self._typed(mask, torch.int64), mask.shape[1]
 
+    def _max_rows(self, n: int) -> None:
+        if not 0 < n <= MAX_TREE:
+            raise SpiffyError(SPIFFY_ESHAPE if n > 0 else SPIFFY_EINVAL, "max_rows %d" % n)
+
     def _layer(self, layer: int):
         if not 0 <= layer < self.n_layers:
             raise IndexError("layer %d of %d" % (layer, self.n_layers))
         return self._layer_refs[layer]
 
     def _elsewhere(self, stream) -> bool:
+        if self._index is None:
+            raise ValueError("the cache is on %s, not on a GPU" % self.device)
         return stream is not None or torch.cuda.current_device() != self._index
 
     def _current(self) -> Optional[int]:
@@ -722,8 +730,12 @@ class PagedCache:
             raise ValueError("rows_k and rows_v are [n_layers, T, Hkv, hd] of the same strides")
         T, L, Hkv = shape[1], self.n_layers, self.cfg.n_kv_heads
         rp, sp = self._ints(row_start, self.n_seqs + 1), self._ints(status, self.n_seqs)
-        stride = self._rows(rows_k[0], Hkv, T)
-        self._rows(rows_v[0], Hkv, T)
+        if shape[2] != Hkv or shape[3] != self.cfg.head_dim or rows_k.dtype != self._dt or rows_v.dtype != self._dt or \
+                rows_k.device != self.device or rows_v.device != self.device:
+            raise ValueError("rows_k and rows_v are [n_layers, T, %d, %d] %s on %s" % (Hkv, self.cfg.head_dim, self._dt, self.device))
+        if T > 0 and (strides[3] != 1 or (Hkv > 1 and strides[2] != self.cfg.head_dim)):
+            raise ValueError("the heads of a row lie side by side")
+        stride = strides[1] if T > 1 else Hkv * self.cfg.head_dim
         mp, words = self._mask(mask, T)
         if node is not None and (node.dtype != torch.int32 or node.device != self.device or tuple(node.shape) != (self.n_seqs,)):
             raise ValueError("node is [n_seqs] int32")
@@ -732,8 +744,7 @@ class PagedCache:
         if self._elsewhere(stream):
             return self._there(stream, self.append, rows_k, rows_v, row_start, mask, node, status, workspace)
         step, k0, v0 = strides[0] * rows_k.element_size(), rows_k.data_ptr(), rows_v.data_ptr()
-        kp = (C.c_void_p * L)(*range(k0, k0 + L * step, step)) if step else (C.c_void_p * L)(*[k0] * L)
-        vp = (C.c_void_p * L)(*range(v0, v0 + L * step, step)) if step else (C.c_void_p * L)(*[v0] * L)
+        kp, vp = self._ptrs(*[k0 + l * step for l in range(L)]), self._ptrs(*[v0 + l * step for l in range(L)])
         ws, wp, wn = self._scratch(self._pages_ws, workspace)
         _check(lib.spiffy_pages_append(self._cfg, self._cache, L, self._layers, kp, vp, stride, rp, T, mp, words,
                                        None if node is None else node.data_ptr(), 1 if node is None or self.n_seqs == 1 else node.stride(0),
@@ -787,6 +798,9 @@ class PagedCache:
         """The n_sel pages of every (sequence, kv head) whose summaries promise the highest scores with the new rows' queries q
         [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; a sequence's first keep_first and last keep_last pages come before all others."""
         T, shape = q.shape[0], (self.n_seqs, self.cfg.n_kv_heads, n_sel)
+        self._max_rows(max_rows)
+        if not (0 < n_sel <= 1 << 22 and 0 <= keep_first < 1 << 31 and 0 <= keep_last < 1 << 31):
+            raise SpiffyError(SPIFFY_EINVAL, "select of %d pages, the first %d and the last %d" % (n_sel, keep_first, keep_last))
         lp, stride, rp = self._layer(layer), self._rows(q, self.cfg.n_q_heads, T), self._ints(row_start, self.n_seqs + 1)
         if out is not None and tuple(out.shape) != shape:
             raise ValueError("out is %s" % (shape,))
@@ -803,9 +817,10 @@ class PagedCache:
     def attend_workspace_bytes(self, max_rows: int) -> int:
         n = self._attn_ws.get(max_rows)
         if n is None:
+            self._max_rows(max_rows)
             n = int(lib.spiffy_tree_attention_workspace_bytes(self._cfg, self._cache, max_rows))
             if n == 0:
-                raise SpiffyError(SPIFFY_ESHAPE if max_rows > 0 else SPIFFY_EINVAL, "spiffy_tree_attention_workspace_bytes")
+                raise SpiffyError(SPIFFY_ESHAPE, "spiffy_tree_attention_workspace_bytes")
             self._attn_ws[max_rows] = n
         return n
 

@@ -247,6 +247,23 @@ def test_offsets_beyond_32_bits():
     p = torch.softmax((k * q.double()).sum(2) * hd ** -0.5, 0)
     _close(got[0], (p[:, :, None] * v).sum(0).cpu(), BF, 1000, "far pages")
     assert torch.equal(cache.summary[0, n_pages + 3, :, 0], rows[0, 384:512, :Hkv].amin(0))
+    # many rows (tiles through LDS), a selection, a fork and its append
+    T = 100
+    q = torch.randn((T, 8, hd), generator=gen, device=DEV).to(BF)
+    z, start, none = torch.zeros((T, 8, hd), dtype=BF, device=DEV), torch.tensor([0, T, T], dtype=torch.int32, device=DEV), torch.zeros((T, 2), dtype=torch.int64, device=DEV)
+    want = torch.einsum("thj,jhd->thd", torch.softmax(torch.einsum("thd,jhd->thj", q.float(), k.float()).double() * hd ** -0.5, 2).float(), v.float())
+    _close(cache.attend(0, q, z, z, start, T, mask=none), want.double().cpu(), BF, 1000, "far pages, many rows")
+    sel = cache.select(0, q, start, T, 8)
+    assert sel[0].tolist() == [list(range(8))] * Hkv and sel[1].tolist() == [[0] + [-1] * 7] * Hkv
+    _close(cache.attend(0, q, z, z, start, T, mask=none, selected=sel), want.double().cpu(), BF, 1000, "far pages, selected")
+    cache.free(torch.tensor([1], dtype=torch.int32, device=DEV))
+    cache.fork(torch.tensor([0], dtype=torch.int32, device=DEV), torch.tensor([1], dtype=torch.int32, device=DEV))
+    cache.append(rows[:, :3, :Hkv], rows[:, :3, Hkv:], torch.tensor([0, 0, 3], dtype=torch.int32, device=DEV))
+    assert cache.table[1, :8].tolist() == [*range(n_pages, n_pages + 7), n_pages + 8] and cache.len.tolist() == [1000, 1003]
+    assert torch.equal(cache.k[0, n_pages + 8, :, :104], cache.k[0, n_pages + 7, :, :104]) and torch.equal(cache.v[0, n_pages + 8, :, 106], rows[0, 2, Hkv:])
+    cache.refs[:100] = 0                                        # pages 0 .. 99 go, and with them the need for the far ones
+    assert cache.compact().item() == n_pages - 100 + 9 and int(cache.table.max()) < n_pages
+    _close(cache.attend(0, q, z, z, start, T, mask=none), want.double().cpu(), BF, 1000, "after compaction")
 
 
 # ---- selection --------------------------------------------------------------------------------------------------------------
@@ -294,6 +311,25 @@ def test_selection_of_equal_infinite_and_nan_scores():
     x.qkv.zero_()
     got = cache.select(0, x.rows(0, DEV)[0], start, 2, 9, keep_first=0, keep_last=2)
     assert got.tolist() == plain.select(0, x.rows(0)[0], x.start, 9, 0, 2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("nodes", [[5, 1], [11, 20], [17, 3], [40, 33], [2, 70]])
+def test_selection_with_summaries_that_are_not_finite(dtype, nodes):
+    """Infinities on one side of a page's bounds: the channel's term is what the formula gives for each query's sign, for every row."""
+    x = Setup(dtype, 4, 2, 24, 4, [300, 160], nodes, seed=sum(nodes), summaries=True)
+    plain = x.plain()
+    plain.summarize()
+    for s, n in ((0, 75), (1, 40)):
+        for i in range(25):
+            j = x.rng.randrange(n)
+            plain.summary[0, plain.table[s][j], x.rng.randrange(2), x.rng.randrange(2), x.rng.randrange(24)] = x.rng.choice([math.inf, -math.inf, math.nan])
+    x.summary = plain.summary
+    cache = _on_gpu(x, dtype)
+    for n_sel in (3, 20):
+        got = cache.select(0, x.rows(0, DEV)[0], torch.tensor(x.start, dtype=torch.int32, device=DEV), max(nodes), n_sel, keep_first=0, keep_last=0)
+        assert got.tolist() == plain.select(0, x.rows(0)[0], x.start, n_sel, 0, 0), n_sel
 
 
 @gpu
@@ -715,6 +751,12 @@ def test_binding_checks_shapes_types_and_strides():
             c.attend(0, *args, **kw)
     with pytest.raises(IndexError):
         c.attend(2, q, k, k, start, 3)
+    for call in (lambda: c.select(0, q, start, 0, 2), lambda: c.select(0, q, start, 1 << 32 | 3, 2), lambda: c.select(0, q, start, 3, 0),
+                 lambda: c.select(0, q, start, 3, 2, keep_last=1 << 32), lambda: c.attend_workspace_bytes(1025), lambda: c.attend_workspace_bytes(1 << 32 | 3)):
+        with pytest.raises(sp.SpiffyError):
+            call()
+    with pytest.raises(ValueError, match="not on a GPU"):      # host memory never reaches a kernel
+        c.attend(0, q, k, k, start, 3)
     for call in (lambda: c.select(0, q, i32(3), 3, 2), lambda: c.select(0, q, start, 3, 2, out=i32(3, 2, 3)), lambda: c.summarize(i32(2)),
                  lambda: c.free(i32(2, 2)), lambda: c.fork(i32(2), i32(3)), lambda: c.fork(i32(2), i32(2), status=i32(1)),
                  lambda: c.append(k, k, start), lambda: c.append(k[None].repeat(2, 1, 1, 1), k[None].repeat(2, 1, 1, 1), start, node=i32(2)),
