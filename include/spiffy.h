@@ -447,14 +447,15 @@ int spiffy_pages_compact(const spiffy_model_cfg *cfg, const spiffy_paged_cache *
                          int32_t *n_used, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Summaries of the pages of every sequence s that hold rows start[s] .. len[s]-1 (start [n_seqs], device; NULL = 0 everywhere): the least
- * and the greatest value of each channel over the rows in use of a page.  Other summaries are left as they were. */
+ * and the greatest value of each channel over the rows in use of a page (NaN is passed over).  Other summaries are left as they were. */
 int spiffy_page_summary(const spiffy_model_cfg *cfg, const spiffy_paged_cache *cache, int32_t n_layers, const spiffy_page_layer *layers,
                         const int32_t *start, void *stream);
 
 /* The pages that a kv head of a sequence is to read.  A page's score is a bound on what any of its keys can score with any of the new
  * rows of the sequence and the query heads of the kv head: max over (row, head) of sum_c max(q_c lo_c, q_c hi_c), summed in 64 bits, so
  * that which of two pages is higher does not depend on the order of a sum.  The first keep_first and the last keep_last pages of a
- * sequence count as the highest, then the higher score, equal ones to the lower index; a score that is NaN is the lowest.
+ * sequence count as the highest, then the higher score, equal ones to the lower index; a (row, head) whose sum is NaN does not
+ * count, and a page of which none counts is the lowest.
  * q: T rows of Hq * hd elements, q_stride apart.  selected [n_seqs, Hkv, n_sel] (device): indices into the sequence's table row,
  * ascending, min(n_sel, pages in use) of them, -1 behind.  A sequence without new rows selects by index alone (every score is
  * the lowest).  n_sel >= 1, keep_first, keep_last >= 0; new rows of a sequence <= SPIFFY_MAX_TREE, max_rows is a bound on them

@@ -513,8 +513,8 @@ Shape shape_of(const Heads& h, int max_rows) {
   s.want = (s.wide ? kWideGroups : target_groups(s.rt)) / (h.Hkv * s.tiles);
   if (s.want < 1) s.want = 1;
   // a sequence of two units or more has more than one full one, so its units are less than twice its blocks over a unit's, and all
-  // blocks over a unit's are `want` at most
-  s.slots = 2ll * s.want + 2;
+  // blocks over a unit's are `want` at most; with one unit wanted no sequence is cut
+  s.slots = s.want == 1 ? 0 : 2ll * s.want + 2;
   return s;
 }
 size_t plan_bytes(const PagedView& c) { return align_up(sizeof(int2) * (size_t)c.n_seqs, 256); }

@@ -156,6 +156,43 @@ def test_what_a_row_does_not_attend_to_does_not_show(dtype, hd, value, n, far):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,ps,S,most", [(BF, 2, 1, 128, 16, 100, 3), (F32, 2, 2, 16, 3, 700, 2), (BF, 4, 1, 64, 8, 130, 20), (BF, 8, 1, 40, 5, 300, 9)])
+def test_many_sequences_in_one_call(dtype, Hq, Hkv, hd, ps, S, most):
+    """More sequences than lanes and than threads, some without rows or without cache, two long ones: attention, summaries and selection."""
+    rng = random.Random(S)
+    lens = [rng.choice([0, 1, rng.randint(1, 60)]) for _ in range(S)]
+    lens[3], lens[S - 2] = 1500, 900
+    nodes = [rng.randint(0, most) for _ in range(S)]
+    nodes[5], nodes[3], nodes[S - 2] = most, 1, 1
+    x = Setup(dtype, Hq, Hkv, hd, ps, lens, nodes, seed=S, summaries=True)
+    rows = x.tree()
+    plain, cache, start = x.plain(), _on_gpu(x, dtype), _ints(x.start)
+    plain.summarize()
+    cache.summarize()
+    assert torch.equal(cache.summary.cpu(), plain.summary)
+    q, k, v = x.rows(0)
+    want = plain.attend(0, q, k, v, x.start, rows, scale=hd ** -0.5)
+    _close(cache.attend(0, *x.rows(0, DEV), start, most, mask=mask_words(rows, 1).to(DEV)), want, dtype, 1600, S)
+    sel = plain.select(0, q, x.start, 4, 1, 1)
+    got = cache.select(0, x.rows(0, DEV)[0], start, most, 4, keep_first=1, keep_last=1)
+    assert got.tolist() == sel
+    want = plain.attend(0, q, k, v, x.start, rows, selected=sel, scale=hd ** -0.5)
+    _close(cache.attend(0, *x.rows(0, DEV), start, most, mask=mask_words(rows, 1).to(DEV), selected=got), want, dtype, 100, (S, "selected"))
+
+
+@gpu
+@pytest.mark.parametrize("dtype,n", [(BF, 5), (BF, 60), (F32, 9)])
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30])
+def test_scales_of_zero_and_below(dtype, n, scale):
+    x = Setup(dtype, 4, 2, 64, 16, [300], [n], seed=n)
+    rows = x.tree()
+    q, k, v = x.rows(0)
+    want = x.plain().attend(0, q, k, v, x.start, rows, scale=scale)
+    got = _on_gpu(x, dtype).attend(0, *x.rows(0, DEV), _ints(x.start), n, mask=mask_words(rows, 1).to(DEV), scale=scale)
+    _close(got, want, dtype, 400, (dtype, n, scale))
+
+
+@gpu
 def test_extreme_scores_and_empty_rows():
     """Scores of +-1e4 (a running maximum that jumps), equal scores, and rows without any key."""
     x = Setup(F32, 2, 1, 64, 16, [100, 0], [20, 3], seed=5, garbage=False)
