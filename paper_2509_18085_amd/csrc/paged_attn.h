@@ -5,7 +5,7 @@
 namespace spiffy {
 
 constexpr int kAlign = 128;             // keys of a block: units are whole blocks, four wavefronts' steps
-constexpr int kMinBlocks = 2;           // blocks of a unit at least
+constexpr int kMinBlocks = 1;           // blocks of a unit at least (two: one token over 500 rows 13.0 us instead of 11.9, fp32 chains 17.3 instead of 14.1)
 
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ bool finite_bits(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80u) != 0x7f80u; }
@@ -59,25 +59,25 @@ __device__ __forceinline__ int wave_scan(int x) {
   return dpp_add<0x143, 0xC>(x);   // row_bcast:31 to rows 2 and 3
 }
 
-// A workgroup's part of a call: `per` workgroups (kv heads times row tiles) a unit, those of one unit next to each other on one XCD.  Only
-// the workgroups of units that there are take part in the spread over the XCDs: a launch is sized for the most units that the
-// sequences can make.
+// A workgroup's part of a call.  (unit, kv head) after (unit, kv head) goes to the next XCD (workgroup ids go round the eight of them), with all
+// its row tiles, which read the same keys: units differ in size, and a range of them to each XCD would not end together (64 sequences of
+// 64 to 16384 rows: 185 us so, 179 this way; calls of equal units are 2% slower).
 struct Place {
-  int unit, part;                       // unit -1: none
+  int unit, kvh, tile;                  // unit -1: none
 };
-__device__ __forceinline__ Place place_of(int units, int per) {
-  const int active = units * per;
-  if ((int)blockIdx.x >= active) return Place{-1, 0};
-  const int logical = xcd_contiguous(blockIdx.x, active);
-  return Place{logical / per, logical % per};
+__device__ __forceinline__ Place place_of(int units, int kv_heads, int tiles) {
+  const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3, group = j / tiles * 8 + xcd;
+  return group < units * kv_heads ? Place{group / kv_heads, group % kv_heads, j % tiles} : Place{-1, 0, 0};
 }
+// workgroups of a launch for up to so many units
+inline long long grid_of(long long units, int kv_heads, int tiles) { return (units * kv_heads + 7) / 8 * 8 * tiles; }
 
 // This workgroup's unit, found by every thread; s < 0: there is none.  Up to 64 sequences a wavefront finds it by itself, a sequence a
 // lane.  There can be up to one unit a sequence more than `want`.  ONE_ROUND: `want` fills the GPU once, so the units of up to `want`
 // sequences grow until there are no more (16 trees over 3000 to 4100 rows, 32 units wanted: 81 us with the 48 that there were, 55
-// with 32).  part: which of the unit's workgroups.
+// with 32).
 template <bool ONE_ROUND>
-__device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int per, int& part) {
+__device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int tiles, int& kvh, int& tile) {
   __shared__ long long sums[8];
   __shared__ int tmp[8], found[3];
   const int tid = threadIdx.x, lane = tid & 63, threads = blockDim.x, n_seqs = a.c.n_seqs;
@@ -93,8 +93,9 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int p
       at = wave_scan(n);
     }
     const int slot = wave_scan(n > 1 ? n : 0);            // like `at`: up to and with this sequence
-    const Place p = place_of(__builtin_amdgcn_readlane(at, kWave - 1), per);
-    part = p.part;
+    const Place p = place_of(__builtin_amdgcn_readlane(at, kWave - 1), a.h.Hkv, tiles);
+    kvh = p.kvh;
+    tile = p.tile;
     const unsigned long long ends = p.unit < 0 ? 0 : __ballot(at > p.unit);
     const int s = ends ? __ffsll(ends) - 1 : 0;
     u.s = ends ? s : -1;
@@ -126,8 +127,9 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int p
     block_scan(s < n_seqs ? units_of(keys_of(a, s).blocks, most) : 0, tmp, all);
     n_units += all;
   }
-  const Place p = place_of(n_units, per);
-  part = p.part;
+  const Place p = place_of(n_units, a.h.Hkv, tiles);
+  kvh = p.kvh;
+  tile = p.tile;
   int before = 0, slots = 0;
   for (int b = 0; p.unit >= 0 && b < n_seqs; b += threads) {
     const int s = b + tid, n = s < n_seqs ? units_of(keys_of(a, s).blocks, most) : 0;

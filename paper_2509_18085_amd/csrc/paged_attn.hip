@@ -66,9 +66,8 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, grp = lane >> 4;
   const int hd = FAST ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
-  int place;
-  const Unit u = find_unit<(RT > 1)>(a, want, row_tiles * a.h.Hkv, place);
-  const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
+  int kvh, tile;
+  const Unit u = find_unit<(RT > 1)>(a, want, row_tiles, kvh, tile);
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * RT * 16;
@@ -522,7 +521,7 @@ size_t ml_bytes(const Heads& h, const Shape& s) { return align_up(sizeof(float2)
 
 template <typename T, int HDP, int RT, bool FAST>
 hipError_t launch_one(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, int log_ps, hipStream_t st) {
-  const long long grid = ((long long)s.want + a.c.n_seqs) * a.h.Hkv * s.tiles;
+  const long long grid = grid_of((long long)s.want + a.c.n_seqs, a.h.Hkv, s.tiles);
   tree_attn_kernel<T, HDP, RT, FAST><<<(unsigned)grid, 256, 0, st>>>(a, ws, s.want, s.tiles, log_ps);
   return hipGetLastError();
 }
@@ -546,7 +545,7 @@ hipError_t launch_rows(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, 
 
 bool tree_attn_fits(const PagedView& c, const Heads& h, int max_rows) {
   const Shape s = shape_of(h, max_rows);
-  return ((long long)s.want + c.n_seqs) * h.Hkv * s.tiles < 1 << 23;
+  return grid_of((long long)s.want + c.n_seqs, h.Hkv, s.tiles) < 1 << 23;
 }
 size_t tree_attn_workspace_bytes(const PagedView& c, const Heads& h, int max_rows) {
   const Shape s = shape_of(h, max_rows);

@@ -48,9 +48,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
   const int hd = QUAD ? HDP : a.h.hd, ps = c.page_size, g = a.h.Hq / a.h.Hkv;
 
-  int place;
-  const Unit u = find_unit<true>(a, want, row_tiles * a.h.Hkv, place);
-  const int tile = place % row_tiles, kvh = place / row_tiles;      // row tiles of the same keys: neighbours on one XCD
+  int kvh, tile;
+  const Unit u = find_unit<true>(a, want, row_tiles, kvh, tile);
   if (u.s < 0) return;
   if (u.index == 0 && kvh == 0 && tile == 0 && tid == 0) ws.plan[u.s] = make_int2(u.units, u.slot);
   const int R = u.rows.n * g, r0 = tile * ROWS;
@@ -494,7 +493,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 hipError_t launch_tree_wide(const TreeAttnArgs& a, const AttnWs& ws, int want, int row_tiles, hipStream_t st) {
   const int ps = a.c.page_size;
   const unsigned magic = 0xffffffffu / (unsigned)ps;
-  const unsigned grid = (unsigned)(((long long)want + a.c.n_seqs) * a.h.Hkv * row_tiles);
+  const unsigned grid = (unsigned)grid_of((long long)want + a.c.n_seqs, a.h.Hkv, row_tiles);
   const bool quad = ps % (a.h.hd == 64 ? 8 : 4) == 0;
   if (a.h.hd == 128 && quad) tree_wide_kernel<128, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);
   else if (a.h.hd == 64 && quad) tree_wide_kernel<64, true><<<grid, kThreads, 0, st>>>(a, ws, want, row_tiles, magic);

@@ -94,7 +94,7 @@ __device__ __forceinline__ bool finite_value(float x) { return (__float_as_uint(
 // four at once, so no operand needs another lane's data.  Which accumulator is which row does not matter: only the maximum over
 // the rows is wanted, and rows beyond the last repeat it.  0 * inf is not what the bound means: 16 pages with a summary that is
 // not finite are scored element by element instead.
-// Trees of 6 to 16 tokens, 32 heads over 8, 4693 pages: 837 us in fp64 vector code, 55 with four row tiles a wavefront one after the other, ROW_US
+// Trees of 6 to 16 tokens, 32 heads over 8, 4693 pages: 837 us in fp64 vector code, 55 with four row tiles a wavefront one after the other, 41
 // with a wavefront a row tile and the next pieces in flight; the matrix instructions alone are 16 us.
 template <typename T>
 __global__ __launch_bounds__(256) void page_score_kernel(const SelectArgs a, int share) {
