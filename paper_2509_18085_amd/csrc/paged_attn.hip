@@ -207,17 +207,14 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
       }
   };
 
-  // ---- the cache
   const T* pk = reinterpret_cast<const T*>(a.pk);
   const T* pv = reinterpret_cast<const T*>(a.pv);
   const long long row_of_page = (long long)a.h.Hkv * ps;  // rows of k or v from one page to the next
   const int cache_hi = min(hi, u.eff);
   constexpr int BATCH = FAST ? kBatchFast : kBatch;
-  for (int batch = lo; batch < cache_hi; batch += BATCH) {
-    const int end = min(cache_hi, batch + BATCH);
-    const int e0 = FAST ? batch >> log_ps : batch / ps, e1 = FAST ? (end - 1) >> log_ps : (end - 1) / ps;
-    if (batch > lo) __syncthreads();
-    const int len = seq_len(c, u.s);
+  auto entry = [&](int key) { return FAST ? key >> log_ps : key / ps; };
+  auto fill_pages = [&](int batch) {
+    const int end = min(cache_hi, batch + BATCH), e0 = entry(batch), e1 = entry(end - 1), len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += 256) {
       const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
       int id = -1, rows = 0;
@@ -228,8 +225,98 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
       page_id[e - e0] = rows ? id : 0;
       page_rows[e - e0] = rows;
     }
-    if (batch == lo) fill_bits();                         // with the first list: their loads wait together
-    __syncthreads();
+  };
+
+  // ---- the new rows
+  // They come first, for their loads need no page: they, the masks and the first list of pages wait together.
+  const long long first = u.rows.first;
+  auto load_new = [&](int at) {                           // rows beyond the last repeat it
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      load_key(reinterpret_cast<const T*>(a.k) + (first + min(at + 16 * n + l16, u.rows.n - 1)) * a.kv_stride + kvh * hd, n);
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j)
+      load_value(reinterpret_cast<const T*>(a.v) + (first + min(at + 16 * (j >> 2) + 4 * grp + (j & 3), u.rows.n - 1)) * a.kv_stride + kvh * hd, j);
+  };
+  int new_at = max(lo - u.tree0, 0) + wave * STEP;
+  if (new_at < hi - u.tree0) load_new(new_at);
+  if (lo < cache_hi) fill_pages(lo);
+  fill_bits();
+  __syncthreads();
+  for (int at = new_at; at < hi - u.tree0; at += 4 * STEP) {
+    unsigned seen[RT], any = 0;                           // bit x: the row of this lane's column attends to new row at + x
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      seen[t] = (unsigned)(bits[(at >> 6) * (RT * 16) + t * 16 + l16] >> (at & 63)) & (unsigned)((1ull << STEP) - 1);
+      any |= seen[t];
+    }
+    if (!__any(any != 0)) continue;
+    if (at > new_at) load_new(at);
+    unsigned odd = 0;                                     // bit j: this lane's j-th key has values that are not finite, taken for 0 here
+#pragma unroll
+    for (int j = 0; j < 4 * NT; ++j) {
+      const int key = at + 16 * (j >> 2) + 4 * grp + (j & 3);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if (key >= u.rows.n) v[j][p] = vvec_t{};
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+          const bool ok = finite_bits((T)v[j][p][e]);
+          odd |= ok ? 0u : 1u << j;
+          v[j][p][e] = ok ? (T)v[j][p][e] : (T)0.f;
+        }
+      }
+    }
+    pvec_t x[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      f32x4 s[NT];
+      scores(t, s);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(seen[t] >> (16 * n + 4 * grp + i) & 1)) s[n][i] = -INFINITY;
+      x[t] = soften(t, s);
+    }
+    add_values(x);
+    // Zero times NaN is NaN: a value that is not finite is added key by key, only in the columns that attend to the key.
+    if (__any(odd != 0)) {
+#pragma unroll 1
+      for (int y = 0; y < STEP; ++y) {
+        const int owner = y >> 2 & 3, slot = (y >> 4) * 4 + (y & 3);
+        if (!__any(grp == owner && (odd >> slot & 1))) continue;
+        const T* row = reinterpret_cast<const T*>(a.v) + (first + min(at + y, u.rows.n - 1)) * a.kv_stride + kvh * hd;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int ch = p * 16 * VW + l16 * VW;
+          const vvec_t z = grp == owner && (FAST || ch < hd) ? *reinterpret_cast<const vvec_t*>(row + ch) : vvec_t{};
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            pvec_t w;
+#pragma unroll
+            for (int j = 0; j < 4 * NT; ++j) w[j] = j != slot || finite_bits((T)z[e]) ? (T)0.f : (T)z[e];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+              const f32x4 more = multiply(w, x[t], f32x4{0.f, 0.f, 0.f, 0.f});
+              const bool mine = seen[t] >> y & 1;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[t][p][e][i] = mine ? o[t][p][e][i] + more[i] : o[t][p][e][i];
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // ---- the cache
+  for (int batch = lo; batch < cache_hi; batch += BATCH) {
+    const int end = min(cache_hi, batch + BATCH), e0 = entry(batch);
+    if (batch > lo) {
+      __syncthreads();
+      fill_pages(batch);
+      __syncthreads();
+    }
     if constexpr (FAST) {
       int have[NT];                                       // rows of the tiles; they and where the tiles lie are the same in all lanes
       long long where[NT];
@@ -319,79 +406,6 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
           x[t] = soften(t, s);
         }
         add_values(x);
-      }
-    }
-  }
-
-  // ---- the new rows
-  if (cache_hi <= lo) fill_bits();
-  __syncthreads();
-  for (int at = max(lo - u.tree0, 0) + wave * STEP; at < hi - u.tree0; at += 4 * STEP) {
-    unsigned seen[RT], any = 0;                           // bit x: the row of this lane's column attends to new row at + x
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      seen[t] = (unsigned)(bits[(at >> 6) * (RT * 16) + t * 16 + l16] >> (at & 63)) & (unsigned)((1ull << STEP) - 1);
-      any |= seen[t];
-    }
-    if (!__any(any != 0)) continue;
-    const long long first = u.rows.first;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-      load_key(reinterpret_cast<const T*>(a.k) + (first + min(at + 16 * n + l16, u.rows.n - 1)) * a.kv_stride + kvh * hd, n);
-    unsigned odd = 0;                                     // bit j: this lane's j-th key has values that are not finite, taken for 0 here
-#pragma unroll
-    for (int j = 0; j < 4 * NT; ++j) {
-      const int key = at + 16 * (j >> 2) + 4 * grp + (j & 3);
-      load_value(reinterpret_cast<const T*>(a.v) + (first + min(key, u.rows.n - 1)) * a.kv_stride + kvh * hd, j);
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        if (key >= u.rows.n) v[j][p] = vvec_t{};
-#pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const bool ok = finite_bits((T)v[j][p][e]);
-          odd |= ok ? 0u : 1u << j;
-          v[j][p][e] = ok ? (T)v[j][p][e] : (T)0.f;
-        }
-      }
-    }
-    pvec_t x[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      f32x4 s[NT];
-      scores(t, s);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(seen[t] >> (16 * n + 4 * grp + i) & 1)) s[n][i] = -INFINITY;
-      x[t] = soften(t, s);
-    }
-    add_values(x);
-    // Zero times NaN is NaN: a value that is not finite is added key by key, only in the columns that attend to the key.
-    if (__any(odd != 0)) {
-#pragma unroll 1
-      for (int y = 0; y < STEP; ++y) {
-        const int owner = y >> 2 & 3, slot = (y >> 4) * 4 + (y & 3);
-        if (!__any(grp == owner && (odd >> slot & 1))) continue;
-        const T* row = reinterpret_cast<const T*>(a.v) + (first + min(at + y, u.rows.n - 1)) * a.kv_stride + kvh * hd;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int ch = p * 16 * VW + l16 * VW;
-          const vvec_t z = grp == owner && (FAST || ch < hd) ? *reinterpret_cast<const vvec_t*>(row + ch) : vvec_t{};
-#pragma unroll
-          for (int e = 0; e < VW; ++e) {
-            pvec_t w;
-#pragma unroll
-            for (int j = 0; j < 4 * NT; ++j) w[j] = j != slot || finite_bits((T)z[e]) ? (T)0.f : (T)z[e];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              const f32x4 more = multiply(w, x[t], f32x4{0.f, 0.f, 0.f, 0.f});
-              const bool mine = seen[t] >> y & 1;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[t][p][e][i] = mine ? o[t][p][e][i] + more[i] : o[t][p][e][i];
-            }
-          }
-        }
       }
     }
   }

@@ -202,25 +202,18 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     }
   };
 
-  // ---- the cache
   const int my_row = tid / PIECES, my_piece = tid % PIECES;
   const bf16_t* pk = reinterpret_cast<const bf16_t*>(a.pk);
   const bf16_t* pv = reinterpret_cast<const bf16_t*>(a.pv);
   const long long row_of_page = (long long)a.h.Hkv * ps;
   const int cache_hi = min(hi, u.eff);
   const int batch_keys = (int)min((long long)(kWideEntries - 2) * ps, (long long)kWideKeys);
-  for (int batch = lo; batch < cache_hi; batch += batch_keys) {
-    const int end = min(cache_hi, batch + batch_keys);
-    auto entry = [&](int key) {                           // key / ps: the product is at most one too low
-      const int e = (int)__umulhi((unsigned)key, magic);
-      return key - e * ps >= ps ? e + 1 : e;
-    };
-    const int e0 = entry(batch), e1 = entry(end - 1);
-    __syncthreads();
-    if (tid == 0) s_bad = end;
-    if (batch == lo && tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
-    __syncthreads();
-    const int len = seq_len(c, u.s);
+  auto entry = [&](int key) {                             // key / ps: the product is at most one too low
+    const int e = (int)__umulhi((unsigned)key, magic);
+    return key - e * ps >= ps ? e + 1 : e;
+  };
+  auto fill_pages = [&](int batch) {                      // s_bad holds the batch's end
+    const int end = min(cache_hi, batch + batch_keys), e0 = entry(batch), e1 = entry(end - 1), len = seq_len(c, u.s);
     for (int e = e0 + tid; e <= e1; e += kThreads) {
       const int slot = a.selected ? a.selected[((long long)u.s * a.h.Hkv + kvh) * a.n_sel + e] : e;
       int id = -1, rows = 0;
@@ -232,8 +225,100 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       s_page[e - e0] = make_int2(QUAD ? (rows ? id * a.h.Hkv : 0) + kvh : id, rows);
       if (rows < ps) atomicMin(&s_bad, e * ps + rows);
     }
-    if (batch == lo) fill_bits();                         // with the first list: their loads wait together
+  };
+
+  // ---- the new rows
+  // They come first, for their loads need no page: they, the masks and the first list of pages wait together.
+  const long long first = u.rows.first;
+  bf16x8 nk[RPT], nv[RPT];
+  auto load_new = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const int r = my_row + i * RSTEP;
+      nk[i] = nv[i] = bf16x8{};
+      if (at + r < u.rows.n && my_piece * 8 < hd) {
+        const long long from = (first + at + r) * a.kv_stride + kvh * hd + my_piece * 8;
+        nk[i] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.k) + from);
+        nv[i] = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.v) + from);
+      }
+    }
+  };
+  const int new_at = max(lo - u.tree0, 0);                // whole words: units begin at multiples of 128
+  if (new_at < hi - u.tree0) load_new(new_at);
+  if (tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
+  if (tid < kTile / 32) s_odd[tid] = 0;
+  if (tid == 0) s_bad = min(cache_hi, lo + batch_keys);
+  __syncthreads();
+  if (lo < cache_hi) fill_pages(lo);
+  fill_bits();
+  __syncthreads();
+  for (int at = new_at; at < hi - u.tree0; at += kTile) {
+    if (!s_any[at >> 6]) continue;
+    if (at > new_at) {
+      load_new(at);
+      __syncthreads();                                    // the tile before is done with
+      if (tid < kTile / 32) s_odd[tid] = 0;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      const int r = my_row + i * RSTEP;
+      bf16x8 y = nv[i];
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool ok = finite_bits((bf16_t)y[e]);
+        odd |= !ok;
+        y[e] = ok ? (bf16_t)y[e] : (bf16_t)0.f;
+      }
+      if (odd) atomicOr(&s_odd[r >> 5], 1u << (r & 31));
+      *reinterpret_cast<bf16x8*>(s_kv + k_at(r, my_piece)) = nk[i];
+      *reinterpret_cast<bf16x8*>(s_kv + 2 * TILEB + v_at(r, my_piece)) = y;
+    }
     __syncthreads();
+    const uint64_t seen = bits[(at >> 6) * ROWS + group * 32 + l32];
+    if (__any(seen != 0)) {
+      f32x16 s;
+      bf16x8 x[2];
+      scores(0, s);
+      hide(s, seen);
+      finish(0, s, x);
+      // values that are not finite, key by key, only in the columns that attend to the key
+      for (unsigned odd = s_odd[part]; odd; odd &= odd - 1) {
+        const int y = __ffs(odd) - 1, key = at + 32 * part + y;      // held by half y / 4 % 2, step y / 16, element 4 (y / 8 % 2) + y % 4
+        const bool mine = seen >> (key & 63) & 1;
+        const bf16_t* from = reinterpret_cast<const bf16_t*>(a.v) + (first + key) * a.kv_stride + kvh * hd;
+        const int slot = 4 * (y >> 3 & 1) + (y & 3);
+#pragma unroll
+        for (int n = 0; n < NN; ++n) {
+          const bf16_t z = 32 * n + l32 < hd && half == (y >> 2 & 1) ? from[32 * n + l32] : (bf16_t)0.f;
+          bf16x8 w, p;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            w[j] = j == slot && !finite_bits(z) ? z : (bf16_t)0.f;
+            p[j] = y >> 4 ? x[1][j] : x[0][j];
+          }
+          f32x16 more;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) more[e] = 0.f;
+          more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p, more, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[n][e] = mine ? o[n][e] + more[e] : o[n][e];
+        }
+      }
+    }
+  }
+
+  // ---- the cache
+  for (int batch = lo; batch < cache_hi; batch += batch_keys) {
+    const int end = min(cache_hi, batch + batch_keys), e0 = entry(batch);
+    __syncthreads();                                      // the new rows' tiles or the last batch's are done with
+    if (batch > lo) {
+      if (tid == 0) s_bad = end;
+      __syncthreads();
+      fill_pages(batch);
+      __syncthreads();
+    }
     const int tiles = (end - batch + kTile - 1) / kTile, bad = s_bad;      // below `bad` every key has a row
     // row of the pool that holds a key, -1: none
     auto find = [&](int key) {
@@ -368,75 +453,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     for (int t = 0; t < tiles; t += 2) {
       turn(t, std::integral_constant<int, 0>{}, sa, sb);
       if (t + 1 < tiles) turn(t + 1, std::integral_constant<int, 1>{}, sb, sa);
-    }
-  }
-
-  // ---- the new rows
-  if (hi > u.tree0) {
-    if (cache_hi <= lo) {
-      if (tid < SPIFFY_MAX_TREE / 64) s_any[tid] = 0;
-      __syncthreads();
-      fill_bits();
-    }
-    __syncthreads();
-    const long long first = u.rows.first;
-    for (int at = max(lo - u.tree0, 0); at < hi - u.tree0; at += kTile) {      // whole words: units begin at multiples of 128
-      if (!s_any[at >> 6]) continue;
-      __syncthreads();                                    // the tile before is done with
-      if (tid < kTile / 32) s_odd[tid] = 0;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < RPT; ++i) {
-        const int r = my_row + i * RSTEP;
-        bf16x8 x = {}, y = {};
-        if (at + r < u.rows.n && my_piece * 8 < hd) {
-          const long long from = (first + at + r) * a.kv_stride + kvh * hd + my_piece * 8;
-          x = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.k) + from);
-          y = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16_t*>(a.v) + from);
-        }
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool ok = finite_bits((bf16_t)y[e]);
-          odd |= !ok;
-          y[e] = ok ? (bf16_t)y[e] : (bf16_t)0.f;
-        }
-        if (odd) atomicOr(&s_odd[r >> 5], 1u << (r & 31));
-        *reinterpret_cast<bf16x8*>(s_kv + k_at(r, my_piece)) = x;
-        *reinterpret_cast<bf16x8*>(s_kv + 2 * TILEB + v_at(r, my_piece)) = y;
-      }
-      __syncthreads();
-      const uint64_t seen = bits[(at >> 6) * ROWS + group * 32 + l32];
-      if (__any(seen != 0)) {
-        f32x16 s;
-        bf16x8 x[2];
-        scores(0, s);
-        hide(s, seen);
-        finish(0, s, x);
-        // values that are not finite, key by key, only in the columns that attend to the key
-        for (unsigned odd = s_odd[part]; odd; odd &= odd - 1) {
-          const int y = __ffs(odd) - 1, key = at + 32 * part + y;      // held by half y / 4 % 2, step y / 16, element 4 (y / 8 % 2) + y % 4
-          const bool mine = seen >> (key & 63) & 1;
-          const bf16_t* from = reinterpret_cast<const bf16_t*>(a.v) + (first + key) * a.kv_stride + kvh * hd;
-          const int slot = 4 * (y >> 3 & 1) + (y & 3);
-#pragma unroll
-          for (int n = 0; n < NN; ++n) {
-            const bf16_t z = 32 * n + l32 < hd && half == (y >> 2 & 1) ? from[32 * n + l32] : (bf16_t)0.f;
-            bf16x8 w, p;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              w[j] = j == slot && !finite_bits(z) ? z : (bf16_t)0.f;
-              p[j] = y >> 4 ? x[1][j] : x[0][j];
-            }
-            f32x16 more;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) more[e] = 0.f;
-            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, p, more, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[n][e] = mine ? o[n][e] + more[e] : o[n][e];
-          }
-        }
-      }
     }
   }
 
