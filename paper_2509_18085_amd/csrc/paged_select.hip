@@ -86,14 +86,12 @@ __global__ __launch_bounds__(256) void page_summary_kernel(const SummaryArgs a) 
 
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ bool finite_value(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-
 // Scores of 16 pages of one (sequence, kv head) a wavefront or `share` of them (1, 2 or 4, which divide the row tiles of 16 among
 // themselves), on fp64 matrix instructions: with q+ = max(q, 0) and q- = min(q, 0) a bound is q+ . hi + q- . lo.  Operand A is 16 rows
 // by 4 channels, B 4 channels by 16 pages; group grp of 16 lanes takes the 16-byte pieces 4 i + grp of a row, element e of all
 // four at once, so no operand needs another lane's data.  Which accumulator is which row does not matter: only the maximum over
-// the rows is wanted, and rows beyond the last repeat it.  0 * inf is not what the bound means: 16 pages with a summary that is
-// not finite are scored element by element instead.
+// the rows is wanted, and rows beyond the last repeat it.  0 * inf is not what the bound means, and shows as NaN: then the 16
+// pages are scored element by element instead.
 // Trees of 6 to 16 tokens, 32 heads over 8, 4693 pages: 837 us in fp64 vector code, 55 with four row tiles a wavefront one after the other, 41
 // with a wavefront a row tile and the next pieces in flight; the matrix instructions alone are 16 us.
 template <typename T>
@@ -134,12 +132,13 @@ __global__ __launch_bounds__(256) void page_score_kernel(const SelectArgs a, int
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float l = to_f32((T)p.least[e]), m = to_f32((T)p.most[e]), v = to_f32((T)p.row[e]);
-        odd |= there && !(finite_value(l) && finite_value(m));
         const bool up = v > 0.f;                           // NaN goes with the negative ones and makes the row's score NaN
         x = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(up ? v : 0.f), (double)m, x, 0, 0, 0);
         y = __builtin_amdgcn_mfma_f64_16x16x4f64((double)(up ? 0.f : v), (double)l, y, 0, 0, 0);
       }
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= there && (x[e] != x[e] || y[e] != y[e]);
     odd = __any(odd);
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = x[e] + y[e] > top ? x[e] + y[e] : top;
