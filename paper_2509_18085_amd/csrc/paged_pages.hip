@@ -2,7 +2,7 @@
 //
 // The reference counts are the whole state of the allocator: a page is free while its count is 0, and calls take the lowest free
 // ones, so what a call does depends on the cache alone, not on the order in which anything ran.  Every call but free has two
-// kernels: a plan by one workgroup (who gets which page: sums over sequences and a scan of the counts, a few microseconds of
+// kernels: a plan by one workgroup (who gets which page: sums over sequences and a scan of the counts, 4 to 10 microseconds of
 // latency) and the copies, which read the plan from the workspace and are bound by memory.
 #include "paged.h"
 
@@ -10,7 +10,7 @@ namespace spiffy {
 
 namespace {
 
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr int kPlanThreads = 512, kPlanWaves = kPlanThreads / 64;
 constexpr int kScanPages = 16;                           // pages that a thread has in flight
 constexpr int kSkip = -2;                                // item_b: nothing to do for this sequence or pair
 
