@@ -625,7 +625,7 @@ class PagedCache:
             raise ValueError("refs is [n_pages], table [n_seqs, max_pages], len [n_seqs]")
         if summary is not None and tuple(summary.shape) != (*k.shape[:3], 2, k.shape[4]):
             raise ValueError("summary is [n_layers, n_pages, Hkv, 2, hd]")
-        self.device, self._dt, self._index = k.device, _tdtype(cfg), k.device.index
+        self.device, self._dt, self._index, self._where = k.device, _tdtype(cfg), k.device.index, k.get_device()
         for t in (k, v) if summary is None else (k, v, summary):
             self._typed(t, self._dt)
         for t in (refs, table, len):
@@ -657,28 +657,31 @@ class PagedCache:
 
     # -- arguments -------------------------------------------------------------------------------------------------------------
 
-    def _typed(self, t: torch.Tensor, dtype) -> Optional[int]:
-        if t.dtype != dtype or t.device != self.device:
+    # These run at every call: plain comparisons first, the reason only once something is wrong.
+
+    def _typed(self, t: torch.Tensor, dtype) -> int:
+        if t.dtype is not dtype or t.get_device() != self._where:
             raise ValueError("expected %s on %s, got %s on %s" % (dtype, self.device, t.dtype, t.device))
         return _ptr(t)
 
     def _ints(self, t: Optional[torch.Tensor], n: int) -> Optional[int]:
         if t is None:
             return None
-        if t.dim() != 1 or t.shape[0] != n:
+        if t.shape != (n,):
             raise ValueError("expected [%d] int32, got %s" % (n, tuple(t.shape)))
         return self._typed(t, torch.int32)
 
     def _rows(self, t: torch.Tensor, heads: int, T: int) -> int:
         """Stride of the rows of [T, heads, hd]; the heads of a row lie side by side."""
-        hd, shape, stride = self.cfg.head_dim, t.shape, t.stride()
-        if len(shape) != 3 or shape[0] != T or shape[1] != heads or shape[2] != hd:
-            raise ValueError("expected [%d, %d, %d], got %s" % (T, heads, hd, tuple(shape)))
-        if t.dtype != self._dt or t.device != self.device:
+        hd = self.cfg.head_dim
+        if t.shape != (T, heads, hd):
+            raise ValueError("expected [%d, %d, %d], got %s" % (T, heads, hd, tuple(t.shape)))
+        if t.dtype is not self._dt or t.get_device() != self._where:
             raise ValueError("expected %s on %s, got %s on %s" % (self._dt, self.device, t.dtype, t.device))
-        if T > 0 and (stride[2] != 1 or (heads > 1 and stride[1] != hd)):
+        row, head, channel = t.stride()
+        if T > 0 and (channel != 1 or (head != hd and heads > 1)):
             raise ValueError("the heads of a row lie side by side")
-        return stride[0] if T > 1 else heads * hd             # of one row torch may say anything
+        return row if T > 1 else heads * hd                   # of one row torch may say anything
 
     def _mask(self, mask: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
         if mask is None:
@@ -713,9 +716,14 @@ class PagedCache:
                 return call(*args, **kw)
 
     def _scratch(self, n: int, workspace: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int, int]:
+        """The workspace (it has to live until the call is made), its aligned address and its bytes from there."""
         if workspace is None:
-            workspace = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
-        return (workspace, *_ws(workspace))
+            workspace = self.refs.new_empty(n + 256, dtype=torch.uint8)
+        elif workspace.get_device() != self._where:
+            raise ValueError("the workspace is on %s, the cache on %s" % (workspace.device, self.device))
+        p = workspace.data_ptr()
+        off = -p % 256
+        return workspace, p + off, workspace.numel() * workspace.element_size() - off
 
     # -- pages -----------------------------------------------------------------------------------------------------------------
 
@@ -778,7 +786,7 @@ class PagedCache:
         if self._elsewhere(stream):
             return self._there(stream, self.compact, n_used, workspace)
         if n_used is None:
-            n_used = torch.empty(1, dtype=torch.int32, device=self.device)
+            n_used = self.refs.new_empty(1)
         up = self._ints(n_used, 1)
         ws, wp, wn = self._scratch(self._pages_ws, workspace)
         _check(lib.spiffy_pages_compact(self._cfg, self._cache, self.n_layers, self._layers, up, wp, wn, self._current()), "spiffy_pages_compact")
@@ -807,7 +815,7 @@ class PagedCache:
         if self._elsewhere(stream):
             return self._there(stream, self.select, layer, q, row_start, max_rows, n_sel, keep_first, keep_last, out, workspace)
         if out is None:
-            out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            out = self.refs.new_empty(shape)
         op = self._typed(out, torch.int32)
         ws, wp, wn = self._scratch(self._select_ws, workspace)
         _check(lib.spiffy_page_select(self._cfg, self._cache, lp, q.data_ptr(), stride, rp, T, max_rows, n_sel, keep_first, keep_last, op,
@@ -845,7 +853,7 @@ class PagedCache:
         if self._elsewhere(stream):
             return self._there(stream, self.attend, layer, q, k, v, row_start, max_rows, mask, selected, scale, out, workspace)
         if out is None:
-            out = torch.empty((T, Hq, hd), dtype=self._dt, device=self.device)
+            out = q.new_empty((T, Hq, hd))
         ws, wp, wn = self._scratch(self.attend_workspace_bytes(max_rows), workspace)
         _check(lib.spiffy_tree_attention(self._cfg, self._cache, lp, q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks, rp, T, max_rows, mp, words,
                                          selp, n_sel, hd ** -0.5 if scale is None else scale, out.data_ptr(), os_, wp, wn, self._current()),
