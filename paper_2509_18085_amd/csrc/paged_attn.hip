@@ -28,6 +28,9 @@ namespace {
 // 83); one row tile leaves room for two or three and wants a second round where lengths differ.
 constexpr int target_groups(int rt) { return rt > 1 ? 256 : 1024; }
 constexpr int kWideGroups = 256;        // the wide kernel: one workgroup a CU
+// Caches of up to 576 keys (fp32: 288) are not cut: one token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us,
+// 450 11.4 / 10.7, 700 11.4 / 12.8; fp32 over 200 13.4 / 12.3, 450 13.6 / 17.8.
+constexpr int kUncutBytes = 1152;       // keys times the element size
 constexpr int kEntries = 1026;          // pages that are looked up at a time
 constexpr int kBatch = 1024;            // ... by keys: pages of one row, and
 constexpr int kBatchFast = 16384;       // pages of 16 rows, from an entry's middle to another's
@@ -521,14 +524,15 @@ struct Shape {
   int rt, tiles, want, rows;
   long long slots;
 };
-Shape shape_of(const Heads& h, int max_rows) {
+// cache_keys: as many as a sequence's cache can hold, or as are selected
+Shape shape_of(const Heads& h, int max_rows, long long cache_keys) {
   Shape s;
   s.rows = max_rows * (h.Hq / h.Hkv);
   s.wide = !h.f32 && h.hd <= 128 && s.rows > 64;
   s.rt = row_tiles_of(h, max_rows);
   s.tiles = cdiv(s.rows, s.wide ? kWideRows : 16 * s.rt);
   s.want = (s.wide ? kWideGroups : target_groups(s.rt)) / (h.Hkv * s.tiles);
-  if (s.want < 1) s.want = 1;
+  if (s.want < 1 || (!s.wide && cache_keys * (h.f32 ? 4 : 2) <= kUncutBytes)) s.want = 1;
   // a sequence of two units or more has more than one full one, so its units are less than twice its blocks over a unit's, and all
   // blocks over a unit's are `want` at most; with one unit wanted no sequence is cut
   s.slots = s.want == 1 ? 0 : 2ll * s.want + 2;
@@ -562,16 +566,17 @@ hipError_t launch_rows(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, 
 }  // namespace
 
 bool tree_attn_fits(const PagedView& c, const Heads& h, int max_rows) {
-  const Shape s = shape_of(h, max_rows);
+  const Shape s = shape_of(h, max_rows, 1ll << 31);
   return grid_of((long long)s.want + c.n_seqs, h.Hkv, s.tiles) < 1 << 23;
 }
 size_t tree_attn_workspace_bytes(const PagedView& c, const Heads& h, int max_rows) {
-  const Shape s = shape_of(h, max_rows);
+  const Shape s = shape_of(h, max_rows, 1ll << 31);      // whether pages are selected is the call's matter: the larger of both
   return plan_bytes(c) + ml_bytes(h, s) + sizeof(float) * (size_t)s.slots * h.Hkv * s.rows * h.hd;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
-  const Shape s = shape_of(a.h, a.max_rows);
+  const long long cache = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size;
+  const Shape s = shape_of(a.h, a.max_rows, cache);
   AttnWs ws;
   unsigned char* p = reinterpret_cast<unsigned char*>(a.workspace);
   ws.plan = reinterpret_cast<int2*>(p);
@@ -584,7 +589,6 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   else e = a.h.hd <= 64 ? launch_rows<bf16_t, 64>(a, ws, s, st) : a.h.hd <= 128 ? launch_rows<bf16_t, 128>(a, ws, s, st) : launch_rows<bf16_t, 256>(a, ws, s, st);
   if (e != hipSuccess) return e;
   // no sequence can have more than one unit: nothing to join
-  const long long cache = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size;
   if (s.want == 1 || (cache + kAlign - 1) / kAlign + a.max_rows / kAlign <= kMinBlocks) return hipSuccess;
   // few rows have many partial results each and wait for them: four wavefronts a row; many rows: one
   const dim3 grid(a.rows.T, a.h.Hq);
