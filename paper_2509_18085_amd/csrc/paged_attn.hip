@@ -16,7 +16,7 @@
 //
 // Up to 64 rows a kv head memory is the bound: one token over 131001 rows of 8 kv heads takes 103 us (537 MB, 5.2 TB/s; a large copy reaches 4.9),
 // 8 tokens (two row tiles) 103, 16 (four) 107; 64 sequences of 64 to 16384 rows, a token each, 179 (923 MB).  Short calls are latency: one
-// token over 500 rows 8 us and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time, took 7235 us at the 64 sequences.
+// token over 500 rows 11 us in one piece, over 32 pages of 64 rows 8.4 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time, took 7235 us at the 64 sequences.
 #include "paged_attn.h"
 
 namespace spiffy {
@@ -28,7 +28,7 @@ namespace {
 // 83); one row tile leaves room for two or three and wants a second round where lengths differ.
 constexpr int target_groups(int rt) { return rt > 1 ? 256 : 1024; }
 constexpr int kWideGroups = 256;        // the wide kernel: one workgroup a CU
-// Caches of up to 576 keys (fp32: 288) are not cut: one token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us,
+// Calls of up to 576 keys a sequence (fp32: 288) are not cut: one token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us,
 // 450 11.4 / 10.7, 700 11.4 / 12.8; fp32 over 200 13.4 / 12.3, 450 13.6 / 17.8.
 constexpr int kUncutBytes = 1152;       // keys times the element size
 constexpr int kEntries = 1026;          // pages that are looked up at a time
@@ -532,7 +532,7 @@ Shape shape_of(const Heads& h, int max_rows, long long cache_keys) {
   s.rt = row_tiles_of(h, max_rows);
   s.tiles = cdiv(s.rows, s.wide ? kWideRows : 16 * s.rt);
   s.want = (s.wide ? kWideGroups : target_groups(s.rt)) / (h.Hkv * s.tiles);
-  if (s.want < 1 || (!s.wide && cache_keys * (h.f32 ? 4 : 2) <= kUncutBytes)) s.want = 1;
+  if (s.want < 1 || (!s.wide && (cache_keys + max_rows) * (h.f32 ? 4 : 2) <= kUncutBytes)) s.want = 1;
   // a sequence of two units or more has more than one full one, so its units are less than twice its blocks over a unit's, and all
   // blocks over a unit's are `want` at most; with one unit wanted no sequence is cut
   s.slots = s.want == 1 ? 0 : 2ll * s.want + 2;
