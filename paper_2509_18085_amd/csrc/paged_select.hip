@@ -2,6 +2,8 @@
 //
 // For channel bounds lo <= k <= hi of a page, q . k <= sum_c max(q_c lo_c, q_c hi_c) for each of its keys, and max(q lo, q hi) is q hi
 // where q > 0 and q lo elsewhere.
+#include <cfloat>
+
 #include "paged.h"
 
 namespace spiffy {
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(256) void page_score_kernel(const SelectArgs a, int
     if (part) return;
     for (int w = 1; w < share; ++w) top = s_top[wave + w][l16] > top ? s_top[wave + w][l16] : top;
   }
-  if (!there) top = -INFINITY;
+  top = there ? fmin(top, DBL_MAX) : -INFINITY;           // an infinite bound stays below the pages that are always taken
   if (slot < a.keep_first || slot >= used - a.keep_last) top = INFINITY;
   if (grp == 0 && slot < used) a.scores[((long long)s * a.h.Hkv + kvh) * c.max_pages + slot] = top;
 }

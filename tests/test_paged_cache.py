@@ -351,6 +351,19 @@ def test_selection_of_equal_infinite_and_nan_scores():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,nodes", [(BF, 1), (BF, 40), (F32, 3)])
+def test_pages_that_are_always_taken_come_before_infinite_bounds(dtype, nodes):
+    """Bounds of +inf on every page: the first and the last pages are taken all the same, then the lowest indices."""
+    x = Setup(dtype, 2, 1, 16, 4, [400], [nodes], seed=5, summaries=True)
+    x.summary[:, :, :, 0], x.summary[:, :, :, 1] = -math.inf, math.inf
+    cache, start = _on_gpu(x, dtype), torch.tensor(x.start, dtype=torch.int32, device=DEV)
+    pick = lambda n, first, last: cache.select(0, x.rows(0, DEV)[0], start, nodes, n, keep_first=first, keep_last=last).tolist()[0][0]
+    assert pick(1, 0, 1) == [99]
+    assert pick(3, 0, 2) == [0, 98, 99]
+    assert pick(4, 1, 1) == [0, 1, 2, 99]
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("nodes", [[5, 1], [11, 20], [17, 3], [40, 33], [2, 70]])
 def test_selection_with_summaries_that_are_not_finite(dtype, nodes):
