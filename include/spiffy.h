@@ -390,8 +390,8 @@ int spiffy_subgraph_search(const int64_t *count, const int32_t *level, int32_t N
  * row of its own sequence (a drafted token: to its ancestors and itself; a state of a block: to the state's rows).
  *
  * Of cfg only n_q_heads (<= 4096), n_kv_heads, head_dim (a multiple of 8, <= 256) and dtype count.  n_seqs <= SPIFFY_MAX_SEQS,
- * n_pages <= 2^30, max_pages <= 2^22, n_sel <= 2^22, rows of the pool below 2^31, of a table row and of a selection up to
- * 2^31 - 2^16, 1 <= T <= SPIFFY_MAX_NEW_ROWS: SPIFFY_ESHAPE beyond.  Buffers that a call writes may not overlap those that it reads. */
+ * n_pages <= 2^30, max_pages <= 2^22, n_sel <= 2^22, the table's entries and the rows of the pool below 2^31, rows of a table row and of a
+ * selection up to 2^31 - 2^16, 1 <= T <= SPIFFY_MAX_NEW_ROWS: SPIFFY_ESHAPE beyond.  Buffers that a call writes may not overlap those that it reads. */
 #define SPIFFY_MAX_SEQS 4096
 #define SPIFFY_MAX_NEW_ROWS (1 << 20)
 #define SPIFFY_MAX_TREE 1024     /* new rows of one sequence in an attention or under a mask */

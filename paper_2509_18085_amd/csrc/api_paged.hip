@@ -26,6 +26,7 @@ Heads heads(const spiffy_model_cfg* c) { return Heads{c->n_q_heads, c->n_kv_head
 int check_sizes(const spiffy_paged_cache* c) {
   if (!c || c->n_pages < 1 || c->page_size < 1 || c->n_seqs < 1 || c->max_pages < 1) return SPIFFY_EINVAL;
   if (c->n_seqs > SPIFFY_MAX_SEQS || c->n_pages > kMaxPoolPages || c->max_pages > kMaxTable) return SPIFFY_ESHAPE;
+  if ((int64_t)c->n_seqs * c->max_pages > INT32_MAX) return SPIFFY_ESHAPE;      // pages of all sequences are counted in 31 bits
   if ((int64_t)c->n_pages * c->page_size > INT32_MAX || (int64_t)c->max_pages * c->page_size > kMaxPositions) return SPIFFY_ESHAPE;
   return SPIFFY_OK;
 }

@@ -731,6 +731,14 @@ def test_page_select_and_summary_refuse():
     assert summary(257, C.byref(_layer()), None) == -2 and summary(1, C.byref(_layer()), DUMMY + 2) == -3
 
 
+def test_tables_of_more_than_31_bits_are_refused():
+    big, fits = (dict(n_seqs=4096, max_pages=m, page_size=1) for m in (1 << 19, (1 << 19) - 1))
+    assert _attend(cache=_host(**big)) == _select(cache=_host(**big)) == -2
+    assert sp.lib.spiffy_page_summary(C.byref(_heads()), C.byref(_host(**big)), 1, C.byref(_layer()), None, None) == -2
+    size = lambda kw: sp.lib.spiffy_pages_workspace_bytes(C.byref(_host(**kw)))
+    assert size(big) == 0 and size(fits) > 0
+
+
 def test_page_operations_refuse():
     one = (C.c_void_p * 1)(DUMMY)
     off = (C.c_void_p * 1)(DUMMY + 8)
