@@ -351,6 +351,14 @@ def test_selection_of_equal_infinite_and_nan_scores():
 
 
 @gpu
+def test_selection_without_new_rows():
+    x = Setup(BF, 2, 1, 16, 4, [400, 9, 0], [2, 1, 1], seed=6, summaries=True)
+    cache, start = _on_gpu(x, BF), torch.zeros(4, dtype=torch.int32, device=DEV)
+    got = cache.select(0, x.rows(0, DEV)[0][:0], start, 2, 4, keep_first=0, keep_last=1).tolist()
+    assert got == [[[0, 1, 2, 99]], [[0, 1, 2, -1]], [[-1] * 4]]
+
+
+@gpu
 @pytest.mark.parametrize("dtype,nodes", [(BF, 1), (BF, 40), (F32, 3)])
 def test_pages_that_are_always_taken_come_before_infinite_bounds(dtype, nodes):
     """Bounds of +inf on every page: the first and the last pages are taken all the same, then the lowest indices."""
