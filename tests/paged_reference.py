@@ -143,8 +143,8 @@ class PlainCache:
                         lo, hi = self.summary[layer, p, h].double()
                         x = torch.where(rows > 0, rows * hi, rows * lo).sum(1)
                         x = max([y for y in x.tolist() if y == y], default=-math.inf)
-                    value.append(math.inf if j < keep_first or j >= used - keep_last else x)
-                best = sorted(sorted(range(used), key=lambda j: (-value[j], j))[:n_sel])
+                    value.append((j < keep_first or j >= used - keep_last, x))
+                best = sorted(sorted(range(used), key=lambda j: (not value[j][0], 0.0 if value[j][0] else -value[j][1], j))[:n_sel])
                 heads.append(best + [-1] * (n_sel - len(best)))
             out.append(heads)
         return out
