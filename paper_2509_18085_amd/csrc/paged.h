@@ -78,7 +78,7 @@ struct SelectArgs {
   NewRows rows;
   int max_rows, n_sel, keep_first, keep_last;
   int32_t* selected;
-  double* scores;           // [n_seqs][Hkv][max_pages]
+  double* scores;           // [n_seqs][Hkv][max_pages], and more behind
 };
 size_t page_select_workspace_bytes(const PagedView& c, const Heads& h);
 hipError_t launch_page_select(const SelectArgs& a, hipStream_t st);

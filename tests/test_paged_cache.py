@@ -351,6 +351,39 @@ def test_selection_of_equal_infinite_and_nan_scores():
 
 
 @gpu
+@pytest.mark.parametrize("hd,nodes", [(128, [1, 30]), (128, [22, 5]), (64, [40, 9]), (256, [7, 24]), (24, [33, 20]), (128, [2, 1])])
+@pytest.mark.parametrize("kind", ["equal", "all equal", "last bit", "cancelling", "large", "infinite", "small"])
+def test_selection_of_nearly_equal_scores(hd, nodes, kind):
+    """Pages whose scores differ by less than fp32 sums tell apart, or not at all, among pages that are far from one another."""
+    x = Setup(BF, 32, 2, hd, 4, [1500, 1203], nodes, seed=hd + nodes[0], summaries=True)
+    plain = x.plain()
+    plain.summarize()
+    rng = torch.Generator().manual_seed(7)
+    for s, n in ((0, 375), (1, 301)):
+        alike = [plain.table[s][j] for j in torch.randperm(n, generator=rng)[:n if kind == "all equal" else n // 2].tolist()]
+        for p in alike[1:]:
+            plain.summary[0, p] = plain.summary[0, alike[0]]
+            h, side, ch = (int(torch.randint(0, m, (1,), generator=rng)) for m in (2, 2, hd))
+            y = plain.summary[0, p, h, side, ch:ch + 1]
+            if kind == "last bit":                              # one channel by its last bit
+                y.view(torch.int16)[0] += int(torch.randint(-1, 2, (1,), generator=rng))
+            elif kind == "cancelling":                          # large terms of both signs: the sum is small beside them
+                plain.summary[0, p, :, :, 0:2] = torch.tensor([4096.0, -4096.0])
+                y.view(torch.int16)[0] += int(torch.randint(-1, 2, (1,), generator=rng))
+            elif kind == "large":
+                plain.summary[0, p, h, 0, ch], plain.summary[0, p, h, 1, ch] = -2.0 ** 70, 2.0 ** 70
+            elif kind == "infinite":
+                y[0] = math.inf if side else -math.inf
+            elif kind == "small":
+                plain.summary[0, p] *= 2.0 ** -128              # subnormal
+    x.summary = plain.summary
+    cache, start = _on_gpu(x, BF), torch.tensor(x.start, dtype=torch.int32, device=DEV)
+    for n_sel, first, last in ((1, 0, 0), (40, 1, 1), (150, 0, 0), (200, 0, 2), (299, 3, 0), (301, 0, 1), (374, 0, 0)):
+        got = cache.select(0, x.rows(0, DEV)[0], start, max(nodes), n_sel, keep_first=first, keep_last=last)
+        assert got.tolist() == plain.select(0, x.rows(0)[0], x.start, n_sel, first, last), (kind, n_sel)
+
+
+@gpu
 def test_selection_without_new_rows():
     x = Setup(BF, 2, 1, 16, 4, [400, 9, 0], [2, 1, 1], seed=6, summaries=True)
     cache, start = _on_gpu(x, BF), torch.zeros(4, dtype=torch.int32, device=DEV)
