@@ -15,7 +15,7 @@
 // its own running maximum and sum; they are joined in LDS, and units of one sequence by a second kernel, always in the same order.
 //
 // Up to 64 rows a kv head memory is the bound: one token over 131001 rows of 8 kv heads takes 103 us (537 MB, 5.2 TB/s; a large copy reaches 4.9),
-// 8 tokens (two row tiles) 103, 16 (four) 107; 64 sequences of 64 to 16384 rows, a token each, 179 (923 MB).  Short calls are latency: one
+// 8 tokens (two row tiles) 103, 16 (four) 109; 64 sequences of 64 to 16384 rows, a token each, 179 (923 MB).  Short calls are latency: one
 // token over 500 rows 11 us in one piece, over 32 pages of 64 rows 8.4 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time, took 7235 us at the 64 sequences.
 #include "paged_attn.h"
 
@@ -23,9 +23,9 @@ namespace spiffy {
 
 namespace {
 
-// Workgroups that the units of a call are to make.  Four row tiles take a CU for one workgroup, two leave no room for a third, and more than one round of them only adds
-// starts and joins (one tree of 16 tokens over 131001 rows, 256 / 512 / 1024: 105 / 116 / 142 us; 16 trees over 3000 to 4100 rows 55 / 65 /
-// 83); one row tile leaves room for two or three and wants a second round where lengths differ.
+// Workgroups that the units of a call are to make.  Four row tiles take a CU for one workgroup, two leave no room for a third, and more than one round of them only
+// adds starts and joins (one tree of 16 tokens over 131001 rows, 256 / 512 / 1024: 105 / 116 / 142 us; two row tiles, one of 3000 rows, 256 / 512:
+// 16.9 / 19.4); one row tile leaves room for two or three and wants a second round where lengths differ.
 constexpr int target_groups(int rt) { return rt > 1 ? 256 : 1024; }
 constexpr int kWideGroups = 256;        // the wide kernel: one workgroup a CU
 // Calls of up to 576 keys a sequence (fp32: 288) are not cut: one token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us,
@@ -44,7 +44,7 @@ template <> struct ValueVec<bf16_t, 4> { typedef bf16x4 type; };
 
 // Wavefronts a SIMD that the registers are to leave room for: accumulators, and keys and values in flight, beside some 60 others
 constexpr int waves_of(int hdp, int rt) {
-  const int regs = rt * hdp / 4 + hdp / 2;
+  const int regs = rt * hdp / 4 + hdp / 2;                // two row tiles of 256 channels: all there are; the steps over new rows spill, those over the cache do not
   return regs <= 64 ? 3 : (regs <= 128 ? 2 : 1);
 }
 
@@ -512,11 +512,21 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeAttnArgs a, co
   store_row(reinterpret_cast<T*>(a.out) + t * a.out_stride + h * hd + pc * 4, o, l);
 }
 
-// Row tiles of a workgroup: enough for all rows of a (sequence, kv head), 64 at most (fp32: 32; more than 128 channels: 16; registers)
-int row_tiles_of(const Heads& h, int max_rows) {
+// Row tiles of a workgroup: enough for all rows of a (sequence, kv head), but
+// - two at most (fp32 with more than 128 channels: one; registers), since four leave a CU one workgroup, whose four wavefronts wait for their loads
+//   at the same time: trees of 16 tokens, 32 heads over 8, four / two, one sequence of 3000 rows 22.6 / 16.8 us, 16 of 700 29.8 / 22.3,
+//   100 of 3000 325 / 297; 24 rows in heads of 256 over 60000 rows, two / one, 48 / 68;
+// - four where the call's keys and values pass 256 MB, which a second reading does not find in a cache, and these workgroups fit in one round:
+//   one sequence of 131001 rows 109 / 122, 16 of 10000 134 / 145, of 4096 58 / 57;
+// - one in calls of one piece while that is no more than kOneTile workgroups: trees of 16 tokens over 200 rows, two / one, 14 sequences 11.9 /
+//   11.6, 8 11.7 / 9.5, 20 14.0 / 18.5.
+constexpr int kOneTile = 512;
+constexpr long long kFarBytes = 1ll << 28;
+int row_tiles_of(const Heads& h, int max_rows, long long lists, long long cache_keys, bool whole) {
   const int rows = max_rows * (h.Hq / h.Hkv);
-  const int most = h.hd > 128 ? 1 : (h.f32 ? 2 : 4);
-  const int need = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+  const bool far = cache_keys >= kFarBytes / (4ll * h.hd) / lists;
+  const int most = h.f32 ? (h.hd > 128 ? 1 : 2) : (h.hd <= 128 && lists <= target_groups(4) && far ? 4 : 2);
+  const int need = rows <= 16 || (whole && lists * cdiv(rows, 16) <= kOneTile) ? 1 : (rows <= 32 ? 2 : 4);
   return need < most ? need : most;
 }
 struct Shape {
@@ -525,14 +535,15 @@ struct Shape {
   long long slots;
 };
 // cache_keys: as many as a sequence's cache can hold, or as are selected
-Shape shape_of(const Heads& h, int max_rows, long long cache_keys) {
+Shape shape_of(const Heads& h, int n_seqs, int max_rows, long long cache_keys) {
   Shape s;
   s.rows = max_rows * (h.Hq / h.Hkv);
   s.wide = !h.f32 && h.hd <= 128 && s.rows > 64;
-  s.rt = row_tiles_of(h, max_rows);
+  const bool whole = !s.wide && (cache_keys + max_rows) * (h.f32 ? 4 : 2) <= kUncutBytes;
+  s.rt = row_tiles_of(h, max_rows, (long long)n_seqs * h.Hkv, cache_keys, whole);
   s.tiles = cdiv(s.rows, s.wide ? kWideRows : 16 * s.rt);
   s.want = (s.wide ? kWideGroups : target_groups(s.rt)) / (h.Hkv * s.tiles);
-  if (s.want < 1 || (!s.wide && (cache_keys + max_rows) * (h.f32 ? 4 : 2) <= kUncutBytes)) s.want = 1;
+  if (s.want < 1 || whole) s.want = 1;
   // a sequence of two units or more has more than one full one, so its units are less than twice its blocks over a unit's, and all
   // blocks over a unit's are `want` at most; with one unit wanted no sequence is cut
   s.slots = s.want == 1 ? 0 : 2ll * s.want + 2;
@@ -555,7 +566,7 @@ hipError_t launch_mode(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, 
 }
 template <typename T, int HDP>
 hipError_t launch_rows(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, hipStream_t st) {
-  constexpr int most = HDP > 128 ? 1 : (sizeof(T) == 4 ? 2 : 4);
+  constexpr int most = sizeof(T) == 4 ? (HDP > 128 ? 1 : 2) : (HDP > 128 ? 2 : 4);
   if constexpr (most >= 4)
     if (s.rt == 4) return launch_mode<T, HDP, 4>(a, ws, s, st);
   if constexpr (most >= 2)
@@ -566,17 +577,17 @@ hipError_t launch_rows(const TreeAttnArgs& a, const AttnWs& ws, const Shape& s, 
 }  // namespace
 
 bool tree_attn_fits(const PagedView& c, const Heads& h, int max_rows) {
-  const Shape s = shape_of(h, max_rows, 1ll << 31);
-  return grid_of((long long)s.want + c.n_seqs, h.Hkv, s.tiles) < 1 << 23;
+  const Shape s = shape_of(h, c.n_seqs, max_rows, 1ll << 31);
+  return grid_of((long long)s.want + c.n_seqs, h.Hkv, s.rt == 4 ? 2 * s.tiles : s.tiles) < 1 << 23;      // two row tiles a workgroup where there are fewer keys
 }
 size_t tree_attn_workspace_bytes(const PagedView& c, const Heads& h, int max_rows) {
-  const Shape s = shape_of(h, max_rows, 1ll << 31);      // whether pages are selected is the call's matter: the larger of both
+  const Shape s = shape_of(h, c.n_seqs, max_rows, 1ll << 31);      // whether pages are selected is the call's matter: the larger of both
   return plan_bytes(c) + ml_bytes(h, s) + sizeof(float) * (size_t)s.slots * h.Hkv * s.rows * h.hd;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st) {
   const long long cache = (long long)(a.selected ? a.n_sel : a.c.max_pages) * a.c.page_size;
-  const Shape s = shape_of(a.h, a.max_rows, cache);
+  const Shape s = shape_of(a.h, a.c.n_seqs, a.max_rows, cache);
   AttnWs ws;
   unsigned char* p = reinterpret_cast<unsigned char*>(a.workspace);
   ws.plan = reinterpret_cast<int2*>(p);
