@@ -197,7 +197,7 @@ __device__ __forceinline__ unsigned long long order_of(double x) {
 // pages above and the first ones equal to it are written in ascending order.  Up to kKeep pages a thread the scores stay in registers.
 constexpr int kPickThreads = 512, kDigit = 12, kBins = 1 << kDigit, kKeep = 8;
 struct PickShared {
-  int hist[kBins];
+  alignas(16) int hist[kBins];
   int tmp[kPickThreads / 64];
   int digit, left, here;
 };
