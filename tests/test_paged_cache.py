@@ -99,6 +99,60 @@ def test_attention_of_trees(case, kind):
 
 
 @gpu
+@pytest.mark.parametrize("case", [
+    (BF, 8, 2, 128, 64, [500, 64, 63, 0, 3000], [13, 16, 1, 9, 7]),
+    (BF, 4, 1, 64, 16, [200, 1], [9, 16]),
+    (BF, 6, 3, 80, 24, [100, 24, 23], [25, 17, 32]),
+    (BF, 28, 4, 128, 128, [300, 2000], [9, 5]),
+    (BF, 3, 1, 40, 5, [700, 3], [20, 21]),
+    (BF, 4, 1, 256, 16, [700, 5], [9, 2]),
+    (F32, 8, 2, 128, 16, [500, 33], [16, 11]),
+], ids=str)
+@pytest.mark.parametrize("kind", ["tree", "full"])
+def test_attention_under_a_long_table(case, kind):
+    """Tables for hundreds of thousands of rows, few of them in use: the variants that are chosen by what a call may have to read."""
+    dtype, Hq, Hkv, hd, ps, lens, nodes = case
+    x = Setup(dtype, Hq, Hkv, hd, ps, lens, nodes, seed=len(lens) + hd, behind=2)
+    entries = -(-(1 << 28) // (4 * hd * Hkv * len(lens) * ps))                # keys and values of 256 MB
+    x.table = torch.nn.functional.pad(x.table, (0, entries), value=-1)
+    rows = x.tree() if kind == "tree" else None
+    want = x.plain().attend(0, *x.rows(0), x.start, rows, scale=hd ** -0.5)
+    cache, start = _on_gpu(x, dtype), torch.tensor(x.start, dtype=torch.int32, device=DEV)
+    out = torch.full((x.T, Hq, hd), 7.0, dtype=dtype, device=DEV)
+    cache.attend(0, *x.rows(0, DEV), start, max(nodes), mask=None if rows is None else mask_words(rows, 1).to(DEV), out=out)
+    n = x.start[-1]
+    assert (out[n:] == 7).all()
+    _close(out[:n], want[:n], dtype, max(lens) + max(nodes), (case[1:], kind))
+
+
+@gpu
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_new_rows_that_are_not_finite_under_a_long_table(value):
+    """As above, with a new row that only some rows attend to."""
+    x = Setup(BF, 4, 1, 128, 16, [100, 40], [16, 12], seed=8)
+    x.table = torch.nn.functional.pad(x.table, (0, 1 << 14), value=-1)
+    rows = [1 << i for i in range(16)] + [1 << i | 1 for i in range(12)]
+    x.qkv[0, 3, 5, ::3] = value                               # the value row of one new row
+    want = x.plain().attend(0, *x.rows(0), x.start, rows, scale=0.1)
+    got = _on_gpu(x, BF).attend(0, *x.rows(0, DEV), torch.tensor(x.start, dtype=torch.int32, device=DEV), 16, mask=mask_words(rows, 1).to(DEV), scale=0.1)
+    keep = [t for t in range(28) if t != 3]
+    _close(got[keep], want[keep], BF, 120, value)
+    assert not torch.isfinite(got[3, :, ::3]).any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("S,n", [(8, 16), (42, 12), (43, 12), (128, 4), (129, 4), (171, 9), (60, 16)])
+def test_many_short_trees(dtype, S, n):
+    """Numbers of workgroups around those at which a workgroup takes more row tiles, 16 (row, head) a tile."""
+    x = Setup(dtype, 16, 4, 64, 16, [7 + 5 * s % 90 for s in range(S)], [n - s % 3 for s in range(S)], seed=S)
+    rows = x.tree()
+    want = x.plain().attend(0, *x.rows(0), x.start, rows, scale=0.125)
+    got = _on_gpu(x, dtype).attend(0, *x.rows(0, DEV), torch.tensor(x.start, dtype=torch.int32, device=DEV), n, mask=mask_words(rows, 1).to(DEV))
+    _close(got, want, dtype, 113, (S, n))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_over_a_long_cache(dtype):
     """Many workgroups a sequence beside sequences of a few rows; the reference is computed in float64 on the GPU."""
