@@ -16,7 +16,8 @@
 //
 // Up to 64 rows a kv head memory is the bound: one token over 131001 rows of 8 kv heads takes 103 us (537 MB, 5.2 TB/s; a large copy reaches 4.9),
 // 8 tokens (two row tiles) 103, 16 (four) 109; 64 sequences of 64 to 16384 rows, a token each, 179 (923 MB).  Short calls are latency: one
-// token over 500 rows 11 us in one piece, over 32 pages of 64 rows 8.4 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time, took 7235 us at the 64 sequences.
+// token over 500 rows 11 us in one piece, over 32 pages of 64 rows 8.4 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time,
+// took 7235 us at the 64 sequences.
 #include "paged_attn.h"
 
 namespace spiffy {
