@@ -102,6 +102,11 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st);
 
 // ---- device -----------------------------------------------------------------------------------------------------------------
 
+// Row of the pool of row `off` of a (page, kv head), these numbered page by page.  Pages may have 2^31 - 1 rows: 64 bits, like what a row
+// is multiplied by.
+__host__ __device__ __forceinline__ long long pool_row(unsigned head_of_page, int page_size, int off) {
+  return (long long)((unsigned long long)head_of_page * (unsigned)page_size + (unsigned)off);
+}
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 __device__ __forceinline__ int seq_len(const PagedView& c, int s) {
   return clamp_int(c.len[s], 0, c.max_pages * c.page_size);      // below 2^31: checked on the host

@@ -354,7 +354,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
         if constexpr (QUAD) {
-          at[i] = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane(page[i]) * (unsigned)(ps * HDP)) + off[i] * HDP;
+          at[i] = pool_row(__builtin_amdgcn_readfirstlane(page[i]), ps, off[i]) * HDP;
         } else {
           const long long r = find(batch + t * kTile + my_row + i * RSTEP);
           at[i] = r >= 0 && my_piece * 8 < hd ? r * hd + my_piece * 8 : -1;

@@ -1,0 +1,82 @@
+"""The paged cache at the ends of what its calls take: pages of more rows than 32-bit offsets reach, scores of any size, calls without rows."""
+import os
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+from paper_2509_18085_amd import build
+from paper_2509_18085_amd import spiffy as sp
+
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+gpu = pytest.mark.gpu
+
+
+def _cfg(dtype, Hq, Hkv, hd):
+    return sp.make_cfg(d=Hq * hd, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=hd, ffn=8, vocab=2, mask_id=1, dtype=dtype)
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _host_program(tmp_path, text):
+    """Compiles a program against the kernels' headers for the host alone and runs it; its output."""
+    source, program = str(tmp_path / "p.hip"), str(tmp_path / "p")
+    with open(source, "w") as f:
+        f.write(text)
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    subprocess.run([hipcc, "-O1", "-std=c++17", "--offload-host-only", "-I", build.CSRC, source, "-o", program], check=True, capture_output=True, timeout=300)
+    return subprocess.run([program], check=True, capture_output=True, text=True, timeout=120).stdout
+
+
+def test_places_in_pages_of_more_than_2_24_rows(tmp_path):
+    """Where a row lies in the pool, against 128-bit arithmetic: pages up to 2^31 - 1 rows, the last kv heads and rows among them."""
+    out = _host_program(tmp_path, r"""
+#include <cstdio>
+#include "paged.h"
+int main() {
+  const int sizes[] = {1, 4, 48, (1 << 24) - 4, 1 << 24, (1 << 24) + 64, 1 << 25, 1 << 26, 1 << 30, 0x7fffffff};
+  const unsigned heads[] = {0, 1, 7, 255, 4095, 1u << 20, 0x7fffffffu, 0xffffffffu};
+  long long n = 0, bad = 0;
+  for (int ps : sizes)
+    for (unsigned h : heads)
+      for (long long off : {0ll, 1ll, (1ll << 24) - 1, 1ll << 24, (1ll << 24) + 5, 1ll << 25, (long long)ps / 2, (long long)ps - 1})
+        if (off < ps && (unsigned __int128)h * ps < ((unsigned __int128)1 << 55)) {
+          ++n;
+          for (int hd : {64, 128}) bad += spiffy::pool_row(h, ps, (int)off) * hd != (long long)(((unsigned __int128)h * ps + off) * hd);
+        }
+  printf("%lld %lld\n", n, bad);
+}
+""")
+    n, bad = (int(x) for x in out.split())
+    assert n > 300 and bad == 0, out
+
+
+@gpu
+@pytest.mark.parametrize("nodes", [1, 20, 70])
+def test_attention_over_one_page_of_more_than_2_24_rows(nodes):
+    """One page of one kv head, 4.3 GB of keys.  All rows but the last 61 have keys and values of zero, so their share of a softmax is
+    their number; the last ones score 16 and some more."""
+    ps, hd = (1 << 24) + 64, 128
+    n, far = ps - 3, ps - 64
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    k, v = (torch.zeros((1, 1, 1, ps, hd), dtype=BF, device=DEV) for _ in range(2))
+    for t in (k, v):
+        t[..., far:, :] = torch.randn((64, hd), generator=gen, device=DEV).to(BF)
+    q = torch.randn((nodes, 1, hd), generator=gen, device=DEV).to(BF)
+    q[..., 0], k[..., far:, 0] = 4.0, 4.0
+    k[..., far:, 1:] *= 0.125
+    k[..., n:, :] = float("nan")
+    v[..., n:, :] = float("nan")
+    new = torch.zeros((nodes, 1, hd), dtype=BF, device=DEV)
+    cache = sp.PagedCache(_cfg(BF, 1, 1, hd), k, v, _ints([1]), _ints([[0]]), _ints([n]))
+    got = cache.attend(0, q, new, new, _ints([0, nodes]), nodes, mask=torch.zeros((nodes, -(-nodes // 64)), dtype=torch.int64, device=DEV), scale=1.0)
+    w = torch.exp(q[:, 0].double() @ k[0, 0, 0, far:n].double().T)
+    want = w @ v[0, 0, 0, far:n].double() / (w.sum(1, keepdim=True) + far)
+    # probabilities and the result are rounded to bf16 (2^-8 of |v| at most, and of the result); fp32 scores are off by less than 1e-4
+    tol = 2.0 ** -8 * v[0, 0, 0, far:n].double().abs().amax() + 2.0 ** -8 * want.abs() + 1e-3
+    assert ((got[:, 0].double() - want).abs() <= tol).all()
+    assert want.abs().amax() > 0.1                           # not what zeros would give
