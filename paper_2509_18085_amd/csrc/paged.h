@@ -107,6 +107,25 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t st);
 __host__ __device__ __forceinline__ long long pool_row(unsigned head_of_page, int page_size, int off) {
   return (long long)((unsigned long long)head_of_page * (unsigned)page_size + (unsigned)off);
 }
+// Pieces at, at + step, .. of the first n of each kv head's `stride` pieces of a page, counted head by head: a page can hold 2^31 pieces and
+// more, and no piece costs a division.  0 <= at < step <= 1024, n >= 1.
+struct HeadPieces {
+  long long n, stride;
+  long long place, in_head;             // place of the present piece in the page, and in its head
+  int heads, rest;                      // what a step is: whole heads, and pieces
+  __host__ __device__ __forceinline__ HeadPieces(long long n, long long stride, int at, int step) : n(n), stride(stride) {
+    const int m = n > 1024 ? 1025 : (int)n;
+    heads = step / m;
+    rest = step - heads * m;
+    in_head = at - at / m * m;
+    place = at / m * stride + in_head;
+  }
+  __host__ __device__ __forceinline__ void next() {
+    in_head += rest;
+    place += heads * stride + rest;
+    if (in_head >= n) in_head -= n, place += stride - n;
+  }
+};
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 __device__ __forceinline__ int seq_len(const PagedView& c, int s) {
   return clamp_int(c.len[s], 0, c.max_pages * c.page_size);      // below 2^31: checked on the host

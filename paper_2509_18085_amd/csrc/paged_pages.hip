@@ -284,11 +284,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(const PagesArgs a, int f
   const long long page_pieces = (long long)a.h.Hkv * ps * seg;
   const u32x4* x = pool + old * page_pieces;
   u32x4* y = pool + page * page_pieces;
-  const int n = rest * seg, stride = ps * seg;
-  for (int u = tid; u < a.h.Hkv * n; u += 256) {
-    const int h = u / n, w = h * stride + (u - h * n);
-    y[w] = x[w];
-  }
+  for (HeadPieces w((long long)rest * seg, (long long)ps * seg, tid, 256); w.place < page_pieces; w.next()) y[w.place] = x[w.place];
   if (part == 0 && a.layers.summary[layer]) {
     u32x4* sum = reinterpret_cast<u32x4*>(a.layers.summary[layer]);
     const int m = a.h.Hkv * 2 * seg;

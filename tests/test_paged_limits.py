@@ -55,6 +55,36 @@ int main() {
     assert n > 300 and bad == 0, out
 
 
+def test_pieces_of_pages_of_more_than_2_31(tmp_path):
+    """The pieces that a thread copies, one after the other, against 128-bit arithmetic: few and many of a head, pages of up to 2^33
+    pieces (128 GB of keys; the first and the last thread walk through them)."""
+    out = _host_program(tmp_path, r"""
+#include <cstdio>
+#include "paged.h"
+int main() {
+  struct { long long heads, n, stride; } cases[] = {
+      {8, 1, 1}, {3, 5, 16}, {4, 255, 256}, {4, 256, 256}, {4, 257, 1024}, {300, 1, 64}, {4096, 2, 16}, {2, 1023, 1024}, {2, 1024, 1024}, {2, 1025, 2048},
+      {8, (1ll << 28) - 16, 1ll << 28}, {8, 1ll << 28, 1ll << 28}, {1, 1ll << 31, (1ll << 31) + 64}, {4, (1ll << 31) - 64, 1ll << 31}};
+  long long walked = 0, bad = 0;
+  for (auto& c : cases)
+    for (int step : {256, 1024})
+      for (int at : {0, 1, 37, 254, 255}) {
+        const bool large = c.heads * c.n > 1 << 22;
+        if (large && (step != 256 || (at && at != 255))) continue;
+        spiffy::HeadPieces w(c.n, c.stride, at, step);
+        for (__int128 u = at; u < (__int128)c.heads * c.n; u += step, w.next()) {
+          ++walked;
+          bad += w.place != (long long)(u / c.n * c.stride + u % c.n);
+        }
+        bad += w.place < c.heads * c.stride;             // the walk ends here
+      }
+  printf("%lld %lld\n", walked, bad);
+}
+""")
+    walked, bad = (int(x) for x in out.split())
+    assert walked > 1 << 26 and bad == 0, out
+
+
 @gpu
 @pytest.mark.parametrize("nodes", [1, 20, 70])
 def test_attention_over_one_page_of_more_than_2_24_rows(nodes):
