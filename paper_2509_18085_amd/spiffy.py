@@ -244,9 +244,10 @@ def alloc_workspace(cfg: ModelCfg, G: int, B: int, P_max: int, device="cuda") ->
 
 
 def _ws(ws: torch.Tensor) -> Tuple[int, int]:
-    p = ws.data_ptr()
+    """Aligned address of a workspace and its bytes from there, none if it ends in front of it."""
+    p = _ptr(ws)
     off = (-p) % 256
-    return p + off, ws.numel() - off
+    return p + off, max(0, ws.numel() * ws.element_size() - off)
 
 
 def _tdtype(cfg: ModelCfg):
@@ -721,9 +722,7 @@ class PagedCache:
             workspace = self.refs.new_empty(n + 256, dtype=torch.uint8)
         elif workspace.get_device() != self._where:
             raise ValueError("the workspace is on %s, the cache on %s" % (workspace.device, self.device))
-        p = workspace.data_ptr()
-        off = -p % 256
-        return workspace, p + off, workspace.numel() * workspace.element_size() - off
+        return (workspace, *_ws(workspace))
 
     # -- pages -----------------------------------------------------------------------------------------------------------------
 

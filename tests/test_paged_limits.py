@@ -110,3 +110,30 @@ def test_attention_over_one_page_of_more_than_2_24_rows(nodes):
     tol = 2.0 ** -8 * v[0, 0, 0, far:n].double().abs().amax() + 2.0 ** -8 * want.abs() + 1e-3
     assert ((got[:, 0].double() - want).abs() <= tol).all()
     assert want.abs().amax() > 0.1                           # not what zeros would give
+
+
+# ---- arguments (no GPU) -----------------------------------------------------------------------------------------------------
+
+
+def _cpu_cache():
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    return sp.PagedCache(_cfg(BF, 4, 2, 16), torch.zeros(2, 5, 2, 8, 16, dtype=BF), torch.zeros(2, 5, 2, 8, 16, dtype=BF), i32(5), i32(3, 4), i32(3),
+                         summary=torch.zeros(2, 5, 2, 2, 16, dtype=BF))
+
+
+def test_workspaces_count_the_bytes_that_they_have():
+    """From the next multiple of 256 on: a view that ends in front of it has none (and no number that reads as a huge one), elements of any
+    size, and no tensor whose elements share memory."""
+    cache, base = _cpu_cache(), torch.zeros(4096, dtype=torch.uint8)
+    skip = -base.data_ptr() % 256
+    for first, n in ((0, 0), (8, 8), (8, 247), (8, 248), (8, 249), (0, 600), (256, 1000)):
+        view = base[skip + first:skip + first + n]
+        want = max(0, n - -first % 256)
+        for p, have in (sp._ws(view), cache._scratch(1, view)[1:]):
+            assert have == want and (n == 0 or p == base.data_ptr() + skip + first + -first % 256), (first, n)
+    wide = torch.zeros(1024, dtype=torch.float32)
+    assert sp._ws(wide)[1] == cache._scratch(1, wide)[2] == 4096 - -wide.data_ptr() % 256
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(4096), base[::2]):
+        for call in (lambda: sp._ws(bad), lambda: cache._scratch(1, bad)):
+            with pytest.raises(ValueError):
+                call()
