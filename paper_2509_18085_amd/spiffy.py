@@ -731,7 +731,7 @@ class PagedCache:
                stream=None) -> None:
         """New rows [n_layers, T, Hkv, hd] to the end of their sequences: all of them, or with mask [T, words] and node [n_seqs] (for
         instance result[:, 0] of n_seqs walks) those on the path to each sequence's accepted node; node -1 appends nothing.
-        status [n_seqs] int32 receives PAGES_*."""
+        status [n_seqs] int32 receives PAGES_*.  Summaries are not written: where pages are selected, summarize(len before the call) follows."""
         shape, strides = rows_k.shape, rows_k.stride()
         if len(shape) != 4 or rows_v.shape != shape or shape[0] != self.n_layers or rows_v.stride() != strides:
             raise ValueError("rows_k and rows_v are [n_layers, T, Hkv, hd] of the same strides")
@@ -803,7 +803,8 @@ class PagedCache:
     def select(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int, n_sel: int, keep_first: int = 0, keep_last: int = 1,
                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The n_sel pages of every (sequence, kv head) whose summaries promise the highest scores with the new rows' queries q
-        [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; a sequence's first keep_first and last keep_last pages come before all others."""
+        [T, Hq, hd], [n_seqs, Hkv, n_sel] int32; a sequence's first keep_first and last keep_last pages come before all others.
+        Summaries are taken as they are: rows that were appended since the last summarize do not count."""
         T, shape = q.shape[0], (self.n_seqs, self.cfg.n_kv_heads, n_sel)
         self._max_rows(max_rows)
         if not (0 < n_sel <= 1 << 22 and 0 <= keep_first < 1 << 31 and 0 <= keep_last < 1 << 31):

@@ -112,6 +112,38 @@ def test_attention_over_one_page_of_more_than_2_24_rows(nodes):
     assert want.abs().amax() > 0.1                           # not what zeros would give
 
 
+@gpu
+def test_the_documented_steps_leave_every_summary_up_to_date():
+    """The example of the README as it stands, its step twice: what `select` will read is the least and greatest key of every page in use."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        lines = f.read().split("\n")
+    first = next(i for i, x in enumerate(lines) if "PagedCache.empty" in x)
+    block = []
+    for x in lines[first:]:
+        if not x.startswith("    "):
+            break
+        block.append(x[4:])
+    step = next(i for i, x in enumerate(block) if x.startswith("mask ="))
+    n_layers, Hq, Hkv, hd, ps, n = 2, 4, 2, 64, 4, 11
+    rows = torch.randn((n_layers, n, Hq + 2 * Hkv, hd), generator=torch.Generator().manual_seed(3)).to(DEV, BF)
+    env = dict(torch=torch, spiffy=sp, cfg=_cfg(BF, Hq, Hkv, hd), n_layers=n_layers, n_pages=40, page_size=ps, n_seqs=2, max_pages=20, layer=1, max_rows=n, n_sel=3,
+               k_rows=rows[:, :, Hq:Hq + Hkv], v_rows=rows[:, :, Hq + Hkv:], q=rows[1, :, :Hq], k=rows[1, :, Hq:Hq + Hkv], v=rows[1, :, Hq + Hkv:],
+               row_start=_ints([0, n, n]), src=_ints([0]), dst=_ints([1]), trees=[([(i, i + 1) for i in range(n - 1)], n)],
+               results=_ints([[n - 1, 0, 0, 0], [-1, 0, 0, 0]]))
+    exec("\n".join(block[:step]), env)
+    for i in range(2):
+        rows.copy_(rows.flip(1) * 1.5)
+        exec("\n".join(block[step:]), env)
+        cache = env["cache"]
+        assert cache.len.tolist() == [n * (i + 2), n]
+        for s, length in enumerate(cache.len.tolist()):
+            for j in range(-(-length // ps)):
+                p, used = int(cache.table[s, j]), min(ps, length - j * ps)
+                keys = cache.k[:, p, :, :used].float()
+                assert torch.equal(cache.summary[:, p].float(), torch.stack([keys.amin(2), keys.amax(2)], 2)), (i, s, j)
+
+
 # ---- arguments (no GPU) -----------------------------------------------------------------------------------------------------
 
 
