@@ -746,10 +746,13 @@ class PagedCache:
         mp, words = self._mask(mask, T)
         if node is not None and (node.dtype != torch.int32 or node.device != self.device or tuple(node.shape) != (self.n_seqs,)):
             raise ValueError("node is [n_seqs] int32")
-        if T == 0:
+        if T == 0 and status is None:
             return
         if self._elsewhere(stream):
             return self._there(stream, self.append, rows_k, rows_v, row_start, mask, node, status, workspace)
+        if T == 0:                                                # one row that no sequence has, for the statuses
+            none = rows_k.new_zeros((L, 1, *shape[2:]))
+            return self.append(none, none, torch.zeros_like(row_start), None if mask is None else mask.new_zeros((1, max(1, words))), node, status, workspace)
         step, k0, v0 = strides[0] * rows_k.element_size(), rows_k.data_ptr(), rows_v.data_ptr()
         kp, vp = self._ptrs(*[k0 + l * step for l in range(L)]), self._ptrs(*[v0 + l * step for l in range(L)])
         ws, wp, wn = self._scratch(self._pages_ws, workspace)

@@ -144,6 +144,29 @@ def test_the_documented_steps_leave_every_summary_up_to_date():
                 assert torch.equal(cache.summary[:, p].float(), torch.stack([keys.amin(2), keys.amax(2)], 2)), (i, s, j)
 
 
+@gpu
+def test_append_of_no_rows_reports():
+    """Every status is written, as by a call in which no sequence has rows; the cache stays."""
+    cache = sp.PagedCache.empty(_cfg(F32, 4, 2, 16), 2, 6, 4, 3, 5, device=DEV)
+    cache.append(*torch.ones((2, 2, 5, 2, 16), device=DEV), _ints([0, 5, 5, 5]))
+    none, kept = torch.zeros((2, 0, 2, 16), device=DEV), [t.clone() for t in (cache.k, cache.v, cache.refs, cache.table, cache.len)]
+    for stream in (None, torch.cuda.Stream()):
+        for start in ([0, 0, 0, 0], [0, 2, 2, 7]):                # row starts are taken within the rows that there are
+            status = _ints([9, 9, 9])
+            torch.cuda.synchronize()
+            cache.append(none, none, _ints(start), status=status, stream=stream)
+            torch.cuda.synchronize()
+            assert status.tolist() == [sp.PAGES_DONE] * 3
+            for words in (0, 1):
+                status.fill_(9)
+                torch.cuda.synchronize()
+                cache.append(none, none, _ints(start), mask=torch.zeros((0, words), dtype=torch.int64, device=DEV), node=_ints([-1, 0, -1]), status=status, stream=stream)
+                torch.cuda.synchronize()
+                assert status.tolist() == [sp.PAGES_DONE, sp.PAGES_BAD, sp.PAGES_DONE]
+    for t, was in zip((cache.k, cache.v, cache.refs, cache.table, cache.len), kept):
+        assert torch.equal(t.nan_to_num(), was.nan_to_num())
+
+
 # ---- arguments (no GPU) -----------------------------------------------------------------------------------------------------
 
 
