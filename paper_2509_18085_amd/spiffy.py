@@ -820,7 +820,8 @@ class PagedCache:
         if out is None:
             out = self.refs.new_empty(shape)
         if T == 0:                                                # no sequence has rows, as a row behind the last sequence says too
-            q, T, stride = q.new_zeros((1, *q.shape[1:])), 1, q.shape[1] * q.shape[2]
+            q, T, stride, row_start = q.new_zeros((1, *q.shape[1:])), 1, q.shape[1] * q.shape[2], torch.zeros_like(row_start)
+            rp = row_start.data_ptr()
         op = self._typed(out, torch.int32)
         ws, wp, wn = self._scratch(self._select_ws, workspace)
         _check(lib.spiffy_page_select(self._cfg, self._cache, lp, q.data_ptr(), stride, rp, T, max_rows, n_sel, keep_first, keep_last, op,

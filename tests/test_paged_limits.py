@@ -167,6 +167,21 @@ def test_append_of_no_rows_reports():
         assert torch.equal(t.nan_to_num(), was.nan_to_num())
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_selection_of_an_empty_batch_takes_row_starts_within_it(dtype):
+    """No rows: by index alone, whatever row_start says, also where a row of zeros would tell pages apart (a page that is not there)."""
+    cache = sp.PagedCache.empty(_cfg(dtype, 4, 2, 16), 1, 9, 4, 2, 8, summaries=True, device=DEV)
+    rows = torch.ones((1, 50, 2, 16), dtype=dtype, device=DEV)
+    cache.append(rows, rows, _ints([0, 30, 32]))
+    cache.summarize()
+    cache.table[0, 1] = -1
+    q = torch.zeros((0, 4, 16), dtype=dtype, device=DEV)
+    for start in ([0, 0, 0], [0, 1, 1], [0, 0, 1], [0, 3, 9]):
+        got = cache.select(0, q, _ints(start), 3, 3, keep_first=1, keep_last=1)
+        assert got.tolist() == [[[0, 1, 7]] * 2, [[0, -1, -1]] * 2], start
+
+
 # ---- arguments (no GPU) -----------------------------------------------------------------------------------------------------
 
 
