@@ -10,6 +10,13 @@ constexpr int kMinBlocks = 1;           // blocks of a unit at least (two: one t
 __device__ __forceinline__ bool finite_bits(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 __device__ __forceinline__ bool finite_bits(bf16_t x) { return (__builtin_bit_cast(unsigned short, x) & 0x7f80u) != 0x7f80u; }
 
+// A probability is exp2 of s * scale - m in one rounding, m the rounded s * scale of a column's highest score: what m was rounded by is the same
+// for all keys of a column and cancels, while it is below 32.  From 2^30 on it could be 64 and more, an infinity or nothing for every key.
+// There fp32 products that are not equal are 64 apart or more, so a key has the highest score or no weight: far_score makes it 0 or minus
+// infinity, for a maximum of 0 (what is not finite comes out as NaN, as it does nearer by).
+constexpr float kFarScore = 0x1p30f;
+__device__ __forceinline__ float far_score(float s, float scale, float m) { return s * scale < m ? -INFINITY : s - s; }
+
 // Weight of a partial result whose maximum is m in one whose maximum is top (logarithms to base 2)
 __device__ __forceinline__ float weight(float m, float top) { return m == top ? 1.f : __builtin_amdgcn_exp2f(m - top); }
 
@@ -127,7 +134,7 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int t
     block_scan(s < n_seqs ? units_of(keys_of(a, s).blocks, most) : 0, tmp, all);
     n_units += all;
   }
-  const Place p = place_of(n_units, a.h.Hkv, tiles);
+  const Place p = place_of(__builtin_amdgcn_readfirstlane(n_units), a.h.Hkv, tiles);
   kvh = p.kvh;
   tile = p.tile;
   int before = 0, slots = 0;
@@ -140,12 +147,12 @@ __device__ __forceinline__ Unit find_unit(const TreeAttnArgs& a, int want, int t
     slots += all_slots;
   }
   __syncthreads();
-  u.s = found[0];
+  u.s = __builtin_amdgcn_readfirstlane(found[0]);
   if (u.s < 0) return u;
   static_cast<Keys&>(u) = keys_of(a, u.s);
   u.units = units_of(u.blocks, most);
-  u.index = p.unit - found[1];
-  u.slot = found[2];
+  u.index = p.unit - __builtin_amdgcn_readfirstlane(found[1]);
+  u.slot = __builtin_amdgcn_readfirstlane(found[2]);
   return u;
 }
 

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   // Running maximum and sum; returns the probabilities.  A column is rescaled only when a score passes its maximum in use by 2^8: with a
   // maximum that is too low by less all is as exact, probabilities are just up to 256 instead of 1.  No column's arithmetic depends
   // on another's.  In bf16 a probability is rounded by up to 2^-8 of itself, as the stored values are; their sum is not.
-  auto soften = [&](int t, const f32x4* s) {
+  auto soften = [&](int t, f32x4* s) {
     float top = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -181,7 +181,15 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
 #pragma unroll
         for (int e = 0; e < VW; ++e) o[t][p][e] *= f;
     }
-    const float base = m[t] == -INFINITY ? 0.f : m[t];    // no score so far: every difference is minus infinity
+    float base = m[t] == -INFINITY ? 0.f : m[t];          // no score so far: every difference is minus infinity
+    if (__any(fabsf(base) >= kFarScore)) {
+      const bool far = fabsf(base) >= kFarScore;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = far ? far_score(s[n][i], scale, base) : s[n][i];
+      base = far ? 0.f : base;
+    }
     pvec_t x;
 #pragma unroll
     for (int n = 0; n < NT; ++n)

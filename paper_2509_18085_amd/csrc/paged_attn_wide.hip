@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   constexpr int PIECES = HDP / 8, RPT = kTile * PIECES / kThreads;      // 16-byte pieces of a row; rows of a thread
   constexpr int RSTEP = kThreads / PIECES, WROWS = kWave / PIECES;      // rows of all threads, of a wavefront
   constexpr int ROWB = HDP * 2, TILEB = kTile * ROWB;
-  __shared__ __align__(16) unsigned char s_kv[4 * TILEB];               // K tiles 0, 1, V tiles 0, 1
+  __shared__ __align__(256) unsigned char s_kv[4 * TILEB];              // K tiles 0, 1, V tiles 0, 1
   __shared__ __align__(16) int2 s_page[kWideEntries];     // page, rows in it
   __shared__ uint64_t bits[(SPIFFY_MAX_TREE / 64) * ROWS];              // [words][ROWS]: what the rows attend to
   __shared__ unsigned long long s_any[SPIFFY_MAX_TREE / 64];
@@ -100,7 +100,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     const int r = 32 * part + 4 * half + ((lane & 15) >> 2), ch = 32 * n + 16 * (l32 >> 4) + 4 * (lane & 3);
     va[n] = lds + 2 * TILEB + v_at(r, ch >> 3) + (ch & 7) * 2;
   }
-  auto k_frag = [&](int buf, int i) { return *(lds_bf16x8_ptr_t)(size_t)(ka[i] + buf * TILEB); };
+  // the last of eight by the fourth's address, whose piece is 8 away (tiles begin at multiples of 256): one register less, and no scratch memory
+  auto k_frag = [&](int buf, int i) { return *(lds_bf16x8_ptr_t)(size_t)((i == 7 ? ka[3] ^ 128 : ka[i]) + buf * TILEB); };
   auto v_half = [&](int buf, int i, int n, int e) {       // keys 16 i + 8 e + 4 half .. + 3 of this half tile, channel 32 n + l32
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(size_t)(va[n] + buf * TILEB + (16 * i + 8 * e) * ROWB));
   };
@@ -119,19 +120,25 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
       if (!(bits >> (8 * (e >> 2) + (e & 3)) & 1)) s[e] = -INFINITY;
   };
   // as in the kernel for few rows: a column is rescaled when a score passes the maximum in use by 2^8.  Returns the maximum in use.
-  auto follow = [&](const f32x16& s) {
+  auto follow = [&](f32x16& s) {
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
     top = reduce_32(top, [](float p, float r) { return fmaxf(p, r); }) * scale;
-    if (__any(top > m + 8.f)) {
+    float base = m;
+    if (__any(top > m + 8.f || fabsf(m) >= kFarScore)) {
       const float m2 = top > m + 8.f ? top : m, f = weight(m, m2);
       m = m2;
       l *= f;
 #pragma unroll
       for (int n = 0; n < NN; ++n) o[n] *= f;
+      base = m == -INFINITY ? 0.f : m;
+      const bool far = fabsf(base) >= kFarScore;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = far ? far_score(s[e], scale, base) : s[e];
+      base = far ? 0.f : base;
     }
-    return m == -INFINITY ? 0.f : m;
+    return base;
   };
   // Probabilities 2 i and 2 i + 1, rounded to bf16 (by up to 2^-8 of themselves, as the stored values are), and the sum of what they are then
   const bf16x2 ones = {(bf16_t)1.f, (bf16_t)1.f};
@@ -463,17 +470,21 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
   }
 
   // ---- results: rows of a lane's column, four channels at a time
+  // Places are worked out again: kept through the loop they are the registers that it lacks.
+  int thread = tid, rows_of_head = g;
+  asm volatile("" : "+v"(thread), "+s"(rows_of_head));
+  const int at_row = (thread >> 6 & 3) * 32 + (thread & 31), out_row = r0 + at_row;
   float sum = reduce_32(l, [](float p, float r) { return p + r; });
   {
     // The upper halves' results go through LDS, 32 channels at a time.
     constexpr int LD = 36;
     static_assert(4 * 32 * LD * sizeof(float) <= sizeof(s_kv) && 4 * 32 * sizeof(float2) <= sizeof(s_page), "join buffers");
-    float* join = reinterpret_cast<float*>(s_kv) + (group * 32 + l32) * LD + 4 * half;
+    float* join = reinterpret_cast<float*>(s_kv) + at_row * LD + 4 * half;
     float2* stat = reinterpret_cast<float2*>(s_page);
     __syncthreads();                                      // tiles and bits are done with
-    if (part == 1 && half == 0) stat[group * 32 + l32] = make_float2(m, sum);
+    if (part == 1 && half == 0) stat[at_row] = make_float2(m, sum);
     __syncthreads();
-    const float2 other = stat[group * 32 + l32];
+    const float2 other = stat[at_row];
     const float top = fmaxf(m, other.x), f = weight(m, top), fo = weight(other.x, top);
 #pragma unroll
     for (int n = 0; n < NN; ++n) {
@@ -494,9 +505,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_wide_kernel(const TreeAttnAr
     sum = sum * f + other.y * fo;
     m = top;
   }
-  if (row >= R) return;
-  const long long at = ((long long)(u.slot + u.index) * a.h.Hkv + kvh) * ws.rows + row;
-  bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + (u.rows.first + row / g) * a.out_stride + (kvh * g + row % g) * hd;
+  if (out_row >= R) return;
+  const long long at = ((long long)(u.slot + u.index) * a.h.Hkv + kvh) * ws.rows + out_row;
+  bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + (u.rows.first + out_row / rows_of_head) * a.out_stride + (kvh * g + out_row % rows_of_head) * hd;
   if (u.units > 1 && half == 0) ws.ml[at] = make_float2(m, sum);
 #pragma unroll
   for (int n = 0; n < NN; ++n)

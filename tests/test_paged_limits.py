@@ -1,11 +1,14 @@
 """The paged cache at the ends of what its calls take: pages of more rows than 32-bit offsets reach, scores of any size, calls without rows."""
+import math
 import os
+import random
 import shutil
 import subprocess
 
 import pytest
 import torch
 
+from paged_reference import Setup, mask_words
 from paper_2509_18085_amd import build
 from paper_2509_18085_amd import spiffy as sp
 
@@ -110,6 +113,52 @@ def test_attention_over_one_page_of_more_than_2_24_rows(nodes):
     tol = 2.0 ** -8 * v[0, 0, 0, far:n].double().abs().amax() + 2.0 ** -8 * want.abs() + 1e-3
     assert ((got[:, 0].double() - want).abs() <= tol).all()
     assert want.abs().amax() > 0.1                           # not what zeros would give
+
+
+# dtype, Hq, Hkv, hd, rows of a page, lengths, new rows: every kernel, in one piece and joined from units
+LARGE = [
+    (BF, 4, 2, 128, 16, [300, 33, 0], [1, 3, 2]),
+    (BF, 4, 2, 128, 16, [3000, 33, 700], [9, 16, 2]),
+    (BF, 4, 1, 80, 24, [900, 100], [13, 5]),
+    (BF, 2, 1, 256, 16, [700, 40], [20, 3]),
+    (BF, 2, 1, 128, 16, [1500, 60], [70, 66]),
+    (BF, 2, 1, 64, 5, [700, 60], [64, 40]),
+    (F32, 4, 2, 64, 24, [700, 33], [9, 3]),
+    (F32, 2, 1, 128, 16, [200, 0], [5, 2]),
+    (F32, 1, 1, 256, 16, [500, 10], [17, 3]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", LARGE, ids=str)
+@pytest.mark.parametrize("size", [28, 29, 31, 36, 115])
+@pytest.mark.parametrize("sign", ["mixed", "negative"])
+def test_scores_of_any_finite_size(case, size, sign):
+    """Scores of 0.75 times 2^size to 2^(size + 1), all exact in fp32 and 2^-7 of that apart or equal: a row gets the mean of the values
+    of its highest keys.  Every highest key's probability is the same number, rounded to bf16 by 2^-8 of itself at most; the mean is rounded once
+    more; the rest are sums in fp32."""
+    dtype, Hq, Hkv, hd, ps, lens, nodes = case
+    x = Setup(dtype, Hq, Hkv, hd, ps, lens, nodes, seed=size + hd)
+    gen, rng = torch.Generator().manual_seed(size), random.Random(size)
+
+    def keys(shape):
+        y = (1 + torch.randint(0, 128, shape, generator=gen) / 128) * 2.0 ** (size - size // 2)
+        return y * (torch.randint(0, 2, shape, generator=gen) * 2 - 1) if sign == "mixed" else -y
+
+    one = torch.zeros_like(x.k)
+    one[..., 3] = keys(x.k.shape[:-1]).to(dtype)
+    x.k = torch.where(x.k.isnan(), x.k, one)
+    x.qkv[:, :, :Hq + Hkv] = 0
+    x.qkv[:, :, :Hq, 3] = 2.0 ** (size // 2)
+    x.qkv[:, :, Hq:Hq + Hkv, 3] = keys((1, x.T, Hkv)).to(dtype)
+    words = -(-max(nodes) // 64)
+    rows = [rng.getrandbits(64 * words) | 1 << i for n in nodes for i in range(n)]
+    want = x.plain().attend(0, *x.rows(0), x.start, rows, scale=0.75)
+    cache = sp.PagedCache(_cfg(dtype, Hq, Hkv, hd), *(t.to(DEV) for t in (x.k, x.v, x.refs, x.table, x.len)))
+    got = cache.attend(0, *x.rows(0, DEV), _ints(x.start), max(nodes), mask=mask_words(rows, words).to(DEV), scale=0.75).double().cpu()
+    assert torch.isfinite(got).all()
+    tol = 2.0 ** -20 * 6 + want.abs() * (0 if dtype == F32 else 2.0 ** -7 * (1 + 2.0 ** -8))
+    assert ((got - want).abs() <= tol).all(), float((got - want).abs().max())
 
 
 @gpu
