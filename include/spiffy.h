@@ -471,7 +471,8 @@ int spiffy_page_select(const spiffy_model_cfg *cfg, const spiffy_paged_cache *ca
  * selected [n_seqs, Hkv, n_sel] (NULL = all pages; as spiffy_page_select leaves it): of the cache only the rows of these pages, in any
  * order, entries outside the pages in use are passed over, each page named once.
  * q rows of Hq * hd, k and v rows of Hkv * hd elements, q_stride / kv_stride apart (one buffer of q | k | v rows will do); out
- * rows out_stride apart; strides are multiples of 16 bytes (SPIFFY_EALIGN).  scale is finite.  max_rows <= SPIFFY_MAX_TREE: a bound
+ * rows out_stride apart; strides are multiples of 16 bytes (SPIFFY_EALIGN).  scale times log2(e) is finite in fp32 (SPIFFY_EINVAL), and so
+ * have to be the sums q . k and what it makes of them: scores of up to 2^127.  max_rows <= SPIFFY_MAX_TREE: a bound
  * on the new rows of a sequence; rows beyond it are left as they were and are no keys.  n_seqs * n_q_heads * max_rows / 16 has to stay below some 2^22
  * (SPIFFY_ESHAPE).
  * Keys and values that a row does not attend to do not show in it, whatever they hold (NaN, infinities).  A row that attends to

@@ -9,6 +9,7 @@ using namespace spiffy;
 namespace {
 
 constexpr int kMaxPoolPages = 1 << 30, kMaxTable = 1 << 22;
+constexpr float kLog2e = 1.4426950408889634f;      // what the kernels' exponentials to base 2 take with the scale
 constexpr int64_t kMaxPositions = (int64_t(1) << 31) - (1 << 16);      // rows of a sequence: kernels count some way past them in 31 bits
 
 inline bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -242,7 +243,7 @@ int spiffy_tree_attention(const spiffy_model_cfg* cfg, const spiffy_paged_cache*
                           void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
   int rc;
   if ((rc = check_heads(cfg)) || (rc = check_cache(cache)) || (rc = check_layers(1, layer, true, false))) return rc;
-  if (!q || !k || !v || !out || max_rows < 1 || (selected && n_sel < 1) || !std::isfinite(scale)) return SPIFFY_EINVAL;
+  if (!q || !k || !v || !out || max_rows < 1 || (selected && n_sel < 1) || !std::isfinite(scale * kLog2e)) return SPIFFY_EINVAL;
   if ((rc = check_rows(row_start, T, mask, mask_words))) return rc;
   if (max_rows > SPIFFY_MAX_TREE || (selected && n_sel > kMaxTable)) return SPIFFY_ESHAPE;
   const Heads h = heads(cfg);

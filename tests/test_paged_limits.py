@@ -1,4 +1,5 @@
 """The paged cache at the ends of what its calls take: pages of more rows than 32-bit offsets reach, scores of any size, calls without rows."""
+import ctypes as C
 import math
 import os
 import random
@@ -256,3 +257,16 @@ def test_workspaces_count_the_bytes_that_they_have():
         for call in (lambda: sp._ws(bad), lambda: cache._scratch(1, bad)):
             with pytest.raises(ValueError):
                 call()
+
+
+def _attend_status(scale):
+    fake = 0x10000                                            # never reached: the call ends at its checks, a workspace of no bytes the last of them
+    return sp.lib.spiffy_tree_attention(C.byref(_cfg(BF, 8, 2, 128)), C.byref(sp.PagedCacheStruct(10, 16, 3, 7, fake, fake, fake)), C.byref(sp.PageLayer(fake, fake, None)),
+                                        fake, 1024, fake, fake, 256, fake, 5, 5, None, 0, None, 0, scale, fake, 1024, fake, 0, None)
+
+
+def test_a_scale_whose_base_2_form_is_not_finite_is_refused():
+    for scale in (2.4e38, -2.4e38, 3.4e38, math.inf, math.nan):
+        assert _attend_status(scale) == sp.SPIFFY_EINVAL, scale
+    for scale in (2.3e38, -2.3e38, 1.0, 0.0, 1e-45):
+        assert _attend_status(scale) == sp.SPIFFY_EWORKSPACE, scale
