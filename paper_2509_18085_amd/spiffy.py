@@ -687,7 +687,7 @@ class PagedCache:
     def _mask(self, mask: Optional[torch.Tensor], T: int) -> Tuple[Optional[int], int]:
         if mask is None:
             return None, 0
-        if mask.dim() != 2 or mask.shape[0] != T:
+        if mask.dim() != 2 or mask.shape[0] != T or (T > 0 and mask.shape[1] < 1):      # no words have no address: none would read as all
             raise ValueError("mask is [T, words] int64")
         return self._typed(mask, torch.int64), mask.shape[1]
 

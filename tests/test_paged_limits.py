@@ -270,3 +270,15 @@ def test_a_scale_whose_base_2_form_is_not_finite_is_refused():
         assert _attend_status(scale) == sp.SPIFFY_EINVAL, scale
     for scale in (2.3e38, -2.3e38, 1.0, 0.0, 1e-45):
         assert _attend_status(scale) == sp.SPIFFY_EWORKSPACE, scale
+
+
+def test_a_mask_of_no_words_is_refused():
+    """It has no address, and without a mask a row attends to every new row of its sequence."""
+    c, start = _cpu_cache(), torch.zeros(4, dtype=torch.int32)
+    q, k, mask = torch.zeros(6, 4, 16, dtype=BF), torch.zeros(6, 2, 16, dtype=BF), torch.zeros(6, 0, dtype=torch.int64)
+    with pytest.raises(ValueError, match="mask"):
+        c.attend(0, q, k, k, start, 3, mask=mask)
+    rows = torch.zeros(2, 6, 2, 16, dtype=BF)
+    with pytest.raises(ValueError, match="mask"):
+        c.append(rows, rows, start, mask=mask, node=torch.zeros(3, dtype=torch.int32))
+    assert c.attend(0, q[:0], k[:0], k[:0], start, 3, mask=mask[:0]).shape == (0, 4, 16)
