@@ -590,17 +590,21 @@ class SeqStepPlan(StepPlan):
         return o
 
 
-def tree_mask(edges, n: int, device="cuda") -> torch.Tensor:
-    """Masks of the n nodes of one draft graph, [n, ceil(n / 64)] int64 (bit i % 64 of word i / 64): every node attends to itself and to all
-    its ancestors.  edges: (parent, child) rows with parent < child, as graph_accept takes them (a sequence or a tensor; host
-    arithmetic: a graph's masks are made once)."""
+def tree_mask(edges, n: int, device="cuda", *, words: Optional[int] = None) -> torch.Tensor:
+    """Masks of the n nodes of one draft graph, [n, words] int64 (bit i % 64 of word i / 64): every node attends to itself and to all
+    its ancestors.  words: ceil(n / 64), or more of them, so that the masks of several graphs lie one behind the other.  edges:
+    (parent, child) rows with parent < child, as graph_accept takes them (a sequence or a tensor; host arithmetic: a graph's
+    masks are made once)."""
+    words = (n + 63) // 64 if words is None else words
+    if 64 * words < n:
+        raise ValueError("%d nodes need more than %d words" % (n, words))
     rows = [1 << i for i in range(n)]
     for p, c in sorted(((int(p), int(c)) for p, c in (edges.tolist() if isinstance(edges, torch.Tensor) else edges)), key=lambda e: e[1]):
         if not 0 <= p < c < n:
             raise ValueError("an edge goes from a node to a later one: got (%d, %d) of %d nodes" % (p, c, n))
         rows[c] |= rows[p]
-    words = [[r >> 64 * w & (1 << 64) - 1 for w in range((n + 63) // 64)] for r in rows]
-    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in words], dtype=torch.int64, device=device).reshape(n, (n + 63) // 64)
+    split = [[r >> 64 * w & (1 << 64) - 1 for w in range(words)] for r in rows]
+    return torch.tensor([[x - (1 << 64) if x >> 63 else x for x in w] for w in split], dtype=torch.int64, device=device).reshape(n, words)
 
 
 # the current stream's handle without the Python object around it (some 3 us a call), where torch has it

@@ -282,3 +282,15 @@ def test_a_mask_of_no_words_is_refused():
     with pytest.raises(ValueError, match="mask"):
         c.append(rows, rows, start, mask=mask, node=torch.zeros(3, dtype=torch.int32))
     assert c.attend(0, q[:0], k[:0], k[:0], start, 3, mask=mask[:0]).shape == (0, 4, 16)
+
+
+def test_masks_of_small_and_large_trees_lie_one_behind_the_other():
+    trees = [([(i, i + 1) for i in range(n - 1)], n) for n in (3, 64, 65, 130, 1)]
+    masks = [sp.tree_mask(e, n, device="cpu", words=3) for e, n in trees]
+    both = torch.cat(masks)
+    assert both.shape == (263, 3)
+    for m, (e, n) in zip(masks, trees):
+        own = sp.tree_mask(e, n, device="cpu")
+        assert torch.equal(m[:, :own.shape[1]], own) and not m[:, own.shape[1]:].any()
+    with pytest.raises(ValueError):
+        sp.tree_mask([], 65, device="cpu", words=1)
