@@ -714,6 +714,8 @@ class PagedCache:
 
     def _there(self, stream, call, *args, **kw):
         """The call on the cache's device and on that stream (a torch stream or a raw handle), whose allocator it then uses."""
+        if getattr(stream, "device", self.device) != self.device:      # torch would make its device the current one
+            raise ValueError("the stream is on %s, the cache on %s" % (stream.device, self.device))
         with torch.cuda.device(self.device):
             if stream is not None and not hasattr(stream, "cuda_stream"):
                 stream = torch.cuda.ExternalStream(int(stream), device=self.device) if int(stream) else torch.cuda.default_stream(self.device)

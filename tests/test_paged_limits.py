@@ -294,3 +294,15 @@ def test_masks_of_small_and_large_trees_lie_one_behind_the_other():
         assert torch.equal(m[:, :own.shape[1]], own) and not m[:, own.shape[1]:].any()
     with pytest.raises(ValueError):
         sp.tree_mask([], 65, device="cpu", words=1)
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Otherwise the call would run on the current stream of the cache's device, in no order with the stream that it was given."""
+    class Elsewhere:
+        device, cuda_stream = torch.device("cuda", 1), 0x10000
+
+    cache, called = _cpu_cache(), []
+    cache.device = torch.device("cuda", 0)
+    with pytest.raises(ValueError, match="stream"):
+        cache._there(Elsewhere(), called.append, 1)
+    assert not called
