@@ -856,7 +856,7 @@ class PagedCache:
             raise ValueError("rows of k and v have the same stride")
         rp, (mp, words), selp, n_sel = self._ints(row_start, self.n_seqs + 1), self._mask(mask, T), None, 0
         if selected is not None:
-            if selected.dim() != 3 or tuple(selected.shape[:2]) != (self.n_seqs, Hkv):
+            if selected.dim() != 3 or tuple(selected.shape[:2]) != (self.n_seqs, Hkv) or selected.shape[2] < 1:      # no entries have no address: none would read as all
                 raise ValueError("selected is [n_seqs, Hkv, n_sel]")
             selp, n_sel = self._typed(selected, torch.int32), selected.shape[2]
         os_ = Hq * hd if out is None else self._rows(out, Hq, T)

@@ -306,3 +306,12 @@ def test_a_stream_of_another_device_is_refused():
     with pytest.raises(ValueError, match="stream"):
         cache._there(Elsewhere(), called.append, 1)
     assert not called
+
+
+def test_a_selection_of_no_pages_is_refused():
+    """It has no address, and without a selection every page is read."""
+    c, start = _cpu_cache(), torch.zeros(4, dtype=torch.int32)
+    q, k, chosen = torch.zeros(6, 4, 16, dtype=BF), torch.zeros(6, 2, 16, dtype=BF), torch.zeros(3, 2, 5, dtype=torch.int32)
+    assert chosen[:, :, :0].contiguous().data_ptr() == 0
+    with pytest.raises(ValueError, match="selected"):
+        c.attend(0, q, k, k, start, 3, selected=chosen[:, :, :0].contiguous())
