@@ -315,3 +315,9 @@ def test_a_selection_of_no_pages_is_refused():
     assert chosen[:, :, :0].contiguous().data_ptr() == 0
     with pytest.raises(ValueError, match="selected"):
         c.attend(0, q, k, k, start, 3, selected=chosen[:, :, :0].contiguous())
+
+
+def test_only_the_widest_kernels_of_the_paged_cache_use_scratch_memory():
+    """bf16 heads of more than 128 channels in two row tiles have more accumulators than registers (they spill around the steps over new rows)."""
+    found = {k for s in build.SOURCES if s.startswith("paged_") for k, n in build.scratch_bytes(s).items() if n}
+    assert len(found) == 2 and all("tree_attn_kernelIDF16bLi256ELi2E" in k for k in found), found
