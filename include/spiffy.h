@@ -452,8 +452,8 @@ int spiffy_page_summary(const spiffy_model_cfg *cfg, const spiffy_paged_cache *c
                         const int32_t *start, void *stream);
 
 /* The pages that a kv head of a sequence is to read.  A page's score is a bound on what any of its keys can score with any of the new
- * rows of the sequence and the query heads of the kv head: max over (row, head) of sum_c max(q_c lo_c, q_c hi_c), summed in 64 bits, so
- * that which of two pages is higher does not depend on the order of a sum.  The first keep_first and the last keep_last pages of a
+ * rows of the sequence and the query heads of the kv head: max over (row, head) of sum_c (q_c hi_c where q_c > 0, q_c lo_c elsewhere),
+ * summed in 64 bits, so that which of two pages is higher does not depend on the order of a sum.  The first keep_first and the last keep_last pages of a
  * sequence count as the highest, then the higher score, equal ones to the lower index; a (row, head) whose sum is NaN does not
  * count, and a page of which none counts is the lowest.
  * q: T rows of Hq * hd elements, q_stride apart.  selected [n_seqs, Hkv, n_sel] (device): indices into the sequence's table row,

@@ -15,8 +15,8 @@
 // its own running maximum and sum; they are joined in LDS, and units of one sequence by a second kernel, always in the same order.
 //
 // Up to 64 rows a kv head memory is the bound: one token over 131001 rows of 8 kv heads takes 103 us (537 MB, 5.2 TB/s; a large copy reaches 4.9),
-// 8 tokens (two row tiles) 103, 16 (four) 109; 64 sequences of 64 to 16384 rows, a token each, 179 (923 MB).  Short calls are latency: one
-// token over 500 rows 11 us in one piece, over 32 pages of 64 rows 8.4 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time,
+// 8 tokens (two row tiles) 103, 16 (four) 109; 64 sequences of 64 to 16384 rows, a token each, 181 (923 MB).  Short calls are latency: one
+// token over 500 rows 10.8 us in one piece (five steps one after the other), over 32 pages of 64 rows 7.8 and 4 of the join.  A workgroup a row and head, reading keys a wavefront at a time,
 // took 7235 us at the 64 sequences.
 #include "paged_attn.h"
 
@@ -29,8 +29,10 @@ namespace {
 // 16.9 / 19.4); one row tile leaves room for two or three and wants a second round where lengths differ.
 constexpr int target_groups(int rt) { return rt > 1 ? 256 : 1024; }
 constexpr int kWideGroups = 256;        // the wide kernel: one workgroup a CU
-// Calls of up to 576 keys a sequence (fp32: 288) are not cut: one token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us,
-// 450 11.4 / 10.7, 700 11.4 / 12.8; fp32 over 200 13.4 / 12.3, 450 13.6 / 17.8.
+// Calls whose tables (or selections) have room for up to 576 keys a sequence (fp32: 288) are not cut; the host, which chooses, does not know the
+// lengths.  One token of one sequence, cut and joined / in one piece, bf16 over 200 rows 11.4 / 8.5 us, 450 11.4 / 10.7, 700 11.4 / 12.8;
+// fp32 over 200 13.4 / 12.3, 450 13.6 / 17.8.  So one token over 500 rows takes 10.8 us under a table of 544 rows, 11.3 under one of 131072; over
+// 200 rows 8.4 and 11.3.
 constexpr int kUncutBytes = 1152;       // keys times the element size
 constexpr int kEntries = 1026;          // pages that are looked up at a time
 constexpr int kBatch = 1024;            // ... by keys: pages of one row, and
@@ -525,8 +527,10 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeAttnArgs a, co
 // - two at most (fp32 with more than 128 channels: one; registers), since four leave a CU one workgroup, whose four wavefronts wait for their loads
 //   at the same time: trees of 16 tokens, 32 heads over 8, four / two, one sequence of 3000 rows 22.6 / 16.8 us, 16 of 700 29.8 / 22.3,
 //   100 of 3000 325 / 297; 24 rows in heads of 256 over 60000 rows, two / one, 48 / 68;
-// - four where the call's keys and values pass 256 MB, which a second reading does not find in a cache, and these workgroups fit in one round:
-//   one sequence of 131001 rows 109 / 122, 16 of 10000 134 / 145, of 4096 58 / 57;
+// - four where the keys and values that the call's tables (or selections) have room for pass 256 MB, which a second reading does not find in a
+//   cache, and these workgroups fit in one round: one sequence of 131001 rows 109 / 122, 16 of 10000 134 / 145, of 4096 58 / 57.  The lengths
+//   are the device's: under a table of 131072 rows that is little used four are taken too (3000 rows 23.3 us, 17.0 under a table that fits; 16
+//   sequences of 700 30.3 and 22.4);
 // - one in calls of one piece while that is no more than kOneTile workgroups: trees of 16 tokens over 200 rows, two / one, 14 sequences 11.9 /
 //   11.6, 8 11.7 / 9.5, 20 14.0 / 18.5.
 constexpr int kOneTile = 512;

@@ -13,9 +13,10 @@
 // LDS and both one more in registers, so a load has a whole step to arrive; one barrier a step.  A row's place in the pool is
 // looked up a step before that, from a list of the unit's pages in LDS: pages of any size.
 //
-// Measured: 128 rows over 131001 rows of 8 kv heads 118 us (537 MB at 4.6 TB/s, memory again), 252 rows 195 to 235 (135 Gflop at 0.6 to
+// Measured: 128 rows over 131001 rows of 8 kv heads 118 us (537 MB at 4.6 TB/s, memory again), 252 rows 186 to 230 (135 Gflop at 0.6 to
 // 0.7 PFLOP/s: a SIMD's matrix pipe works 36% of the time, its vector pipe as much; the clock is 1.9 GHz), 1024 rows of 32 kv heads, 32 states of 32 tokens
-// behind 1024 rows, 38 to 42.  Tried: 256 rows a workgroup, a wavefront 64 keys of each tile (no registers left for reads ahead, 440 us at 252
+// behind 1024 rows, 38 to 41; a prompt of 1024 tokens, 32 heads over 8, behind one row 43.  Tiles of new rows are not pipelined: load, LDS,
+// scores, product, one after the other.  Tried: 256 rows a workgroup, a wavefront 64 keys of each tile (no registers left for reads ahead, 440 us at 252
 // rows); values and keys to LDS in front of a step (222), their loads at its start (231: the eight wavefronts wait for one another's);
 // more or fewer workgroups than CUs (+13 to +30%).
 #include <type_traits>

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(const PagesAr
   }
 }
 
-// A wavefront a row and `layers` layers: 16 bytes a lane, head by head into the page.  Paths of 48 trees of 12 to 40 tokens in 28 layers 11.5 us
+// A wavefront a row and `layers` layers: 16 bytes a lane, head by head into the page.  Paths of 48 trees of 12 to 40 tokens in 28 layers 11.9 us
 // (15.9 with a wavefront a row and layer).
 __global__ __launch_bounds__(256) void append_rows_kernel(const PagesArgs a, int layers) {
   const PagedView& c = a.c;
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const PagesArgs
 }
 
 // One workgroup a (pair, layer, k or v): the rows of the last page; the first layer's also the table row and the references.  48 forks in
-// 28 layers 40 us (176 MB read and written, 4.4 TB/s).
+// 28 layers 41 us (176 MB read and written, 4.3 TB/s).
 __global__ __launch_bounds__(256) void fork_rows_kernel(const PagesArgs a, int first) {
   const PagedView& c = a.c;
   const int i = blockIdx.x, layer = blockIdx.y, part = blockIdx.z, tid = threadIdx.x, ps = c.page_size;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(const PagesA
   }
 }
 
-// 2048 workgroups take (page, layer, k or v) after another.  835 MB read and written in 172 us: the rate of a copy.
+// 2048 workgroups take (page, layer, k or v) after another.  835 MB read and written in 174 us: the rate of a copy.
 __global__ __launch_bounds__(256) void compact_rows_kernel(const PagesArgs a, int first) {
   const PagedView& c = a.c;
   const int tid = threadIdx.x, moves = a.ws.count[0], used = a.ws.count[1];
